@@ -247,6 +247,84 @@ wind_status_t wind_window_first_output(const wind_model_t* m, const void* enc, c
                                        float* top_logp, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Losses of the output layer z = W x + b, without keeping the logits: what scores a transcript, trains the layer, or distils a
+ * small model from a large one.  A row x is the joint's activations at one lattice node or frame (any rows of H values will do).
+ *
+ *   labels   loss_r = ln sum_v exp(z_rv) - z_r,t          t = target[r]
+ *   distill  loss_r = tau^2 sum_k q_rk (ln q_rk - ln p_r,i(r,k)), with q_r the softmax of teacher[r][k] / tau over the entries k
+ *            that are there, i(r, k) = ids[r][k], p_r = softmax of z_r / tau over all outputs
+ *   gradient of sum_r dloss[r] loss_r with regard to x, W and b; with s_r = dloss[r] (distill: tau dloss[r]) and
+ *            g_rv = s_r (p_rv - [sum of the q_rk with i(r, k) = v])  (labels: q is 1 at the target):  dx = g W, dW = g^T x, db = sum_r g_r
+ *
+ * Unlike the decoding calls these only enqueue work (they may be captured into a graph): wind_loss_status waits and returns what
+ * the device found.
+ */
+typedef struct {
+    int32_t n_out, H;          /* outputs (V + 1 of a model), activations */
+    int32_t dtype;             /* wind_dtype_t of x, w, dx and dw */
+    int32_t reserved;
+    const void* w;             /* [n_out, H], rows ldw elements apart (0: the same row for every output) */
+    int64_t ldw;
+    const float* b;            /* [n_out] fp32, or NULL: no bias.  -inf masks an output; at least one has to be left */
+} wind_output_t;
+
+#define WIND_LOSS_MAX_ENTRIES 256
+
+/*
+ * Workspace of the calls below for up to N rows with K teacher's entries each (0: labels); grad: of the gradient's call, else of
+ * the loss's.  `o` as in the call: where W's rows do not start on 16 bytes (address, ldw or H), or the model is fp32, the workspace
+ * has room for W in the kernels' own layout.  The gradient keeps at most a piece of its share of logits (g above) at a time:
+ * 512 MB, or 2048 outputs where that is more.
+ */
+wind_status_t wind_loss_workspace_bytes(const wind_output_t* o, int32_t N, int32_t K, int32_t grad, size_t* bytes);
+
+/*
+ * Loss and log-sum-exp (of z / tau) of N rows against labels.
+ *   x       [N, H], rows ldx elements apart (any distance and alignment; 0: the same row)
+ *   target  [N] int32 in [0, n_out), or -1: a row of padding.  Its loss and lse are 0 and its x is not read (it may hold NaN).
+ *           With another value loss and lse of that row are NaN, no output is read through it and the status is WIND_ERR_INVALID_ARG.
+ *   loss, lse  [N] fp32
+ *   workspace  device memory, 256-byte aligned, at least wind_loss_workspace_bytes(o, N, 0, 0).  Calls sharing a workspace must not
+ *           overlap in time; it carries nothing from one call to the next but the status.
+ * N = 0 is a call without rows.  N <= 2^24, n_out <= 2^24, H <= 65536, else WIND_ERR_UNSUPPORTED.  A target whose output is masked
+ * has loss +inf; non-finite rows of x that are not padding have a loss that is NaN or infinite.
+ */
+wind_status_t wind_label_loss(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* target, int32_t N, float* loss, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradient, for the same o, x and target as the call that wrote lse.
+ *   lse     [N] fp32 (rows of padding are not read)
+ *   dloss   [N] fp32 weights of the rows' losses, or NULL: 1 each (rows of padding are not read)
+ *   dx      [N, H] of the model's dtype, rows lddx >= H elements apart, or NULL: not asked for.  Zero in rows of padding, NaN in rows
+ *           with a target that is no label (which count nowhere else).
+ *   dw      [n_out, H] of the model's dtype, rows lddw >= H elements apart, or NULL;  db  [n_out] fp32, or NULL.  Written, not added to.
+ * Outputs may not overlap inputs.  bf16 models: g is rounded to bf16 (it is an operand of tensor-core products); db, dx and dW are
+ * accumulated in fp32, db from g as it was before that rounding.  Everything else is fp32 throughout.
+ */
+wind_status_t wind_label_loss_grad(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* target, int32_t N, const float* lse,
+                                   const float* dloss, void* dx, int64_t lddx, void* dw, int64_t lddw, float* db, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
+ * The same against a teacher's K best labels, 1 <= K <= WIND_LOSS_MAX_ENTRIES, 0 < tau < inf (lse: of z / tau).
+ *   ids      [N, K] int32 in [0, n_out) in any order, or -1: the teacher has no such entry (wind_window_first_output writes its lists so).
+ *            A label that stands there twice counts with both entries.
+ *   teacher  [N, K] fp32 logits or natural-log probabilities; -inf: probability 0.  Not read where ids is -1.
+ * A row without an entry, or with -inf alone, is a row of padding.  A row with another id is treated like one with another target above.
+ * Workspace: wind_loss_workspace_bytes(o, N, K, 0), for the gradient (o, N, K, 1).
+ */
+wind_status_t wind_distill_loss(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* ids, const float* teacher, int32_t N, int32_t K,
+                                float tau, float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+wind_status_t wind_distill_loss_grad(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* ids, const float* teacher, int32_t N,
+                                     int32_t K, float tau, const float* lse, const float* dloss, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                                     float* db, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Waits for `stream` and returns the status of the last loss or gradient call that used `workspace`: WIND_OK, WIND_ERR_INVALID_ARG
+ * (a target or id that is no label) or WIND_ERR_TIMEOUT. */
+wind_status_t wind_loss_status(const void* workspace, void* stream);
+
+/*
  * Largest workspace, in bytes, that wind_eval_joint_window_static can serve: the size of the
  * scratch array compiled into the library.
  */

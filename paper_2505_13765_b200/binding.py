@@ -34,6 +34,7 @@ EXPORTS = [
     "wind_workspace_bytes", "wind_decode_greedy", "wind_decode_window_greedy", "wind_host_staging_bytes", "wind_decode_greedy_host",
     "wind_eval_joint_window", "wind_window_first_output", "wind_eval_joint_window_static", "wind_profile_decode", "wind_beam_workspace_bytes", "wind_beam_search", "wind_plan_batches", "wind_read_stats", "wind_set_trace", "wind_read_trace", "wind_debug_stall_barrier", "wind_set_kernels", "wind_status_string", "wind_last_cuda_error",
     "wind_set_loop_options", "wind_debug_plan", "wind_debug_cluster_smem", "wind_debug_beam_plan", "wind_bench_joint", "wind_refill_workspace_bytes", "wind_decode_greedy_refill", "wind_debug_loop_kernel",
+    "wind_loss_workspace_bytes", "wind_label_loss", "wind_label_loss_grad", "wind_distill_loss", "wind_distill_loss_grad", "wind_loss_status",
 ]
 
 _vp = C.c_void_p
@@ -90,6 +91,10 @@ class wind_joint_bench_t(C.Structure):
 
 class wind_trace_event_t(C.Structure):
     _fields_ = [("role", C.c_int32), ("phase", C.c_int32), ("event", C.c_int32), ("step", C.c_int32), ("clock", C.c_int64)]
+
+
+class wind_output_t(C.Structure):
+    _fields_ = [("n_out", C.c_int32), ("H", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32), ("w", _vp), ("ldw", C.c_int64), ("b", _vp)]
 
 
 class wind_beam_plan_t(C.Structure):
@@ -163,6 +168,16 @@ def load_library():
     L.wind_debug_beam_plan.restype = i32
     L.wind_bench_joint.argtypes = [mp, i32, i32, i32, _vp, C.c_size_t, _vp, C.POINTER(wind_joint_bench_t)]
     L.wind_bench_joint.restype = i32
+    op, i64 = C.POINTER(wind_output_t), C.c_int64
+    L.wind_loss_workspace_bytes.argtypes = [op, i32, i32, i32, C.POINTER(C.c_size_t)]
+    L.wind_label_loss.argtypes = [op, _vp, i64, _vp, i32, _vp, _vp, _vp, C.c_size_t, _vp]
+    L.wind_label_loss_grad.argtypes = [op, _vp, i64, _vp, i32, _vp, _vp, _vp, i64, _vp, i64, _vp, _vp, C.c_size_t, _vp]
+    L.wind_distill_loss.argtypes = [op, _vp, i64, _vp, _vp, i32, i32, C.c_float, _vp, _vp, _vp, C.c_size_t, _vp]
+    L.wind_distill_loss_grad.argtypes = [op, _vp, i64, _vp, _vp, i32, i32, C.c_float, _vp, _vp, _vp, i64, _vp, i64, _vp, _vp, C.c_size_t, _vp]
+    L.wind_loss_status.argtypes = [_vp, _vp]
+    for name in ("wind_loss_workspace_bytes", "wind_label_loss", "wind_label_loss_grad", "wind_distill_loss", "wind_distill_loss_grad",
+                 "wind_loss_status"):
+        getattr(L, name).restype = i32
     L.wind_status_string.argtypes = [i32]
     L.wind_status_string.restype = C.c_char_p
     L.wind_last_cuda_error.argtypes = []
@@ -510,6 +525,139 @@ def wind_debug_loop_kernel(workspace, stream=None) -> int:
     if st != WIND_OK:
         raise WindError(st)
     return int(which.value)
+
+
+# ---------------------------------------------------------------------------
+# losses of the output layer
+# ---------------------------------------------------------------------------
+WIND_LOSS_MAX_ENTRIES = 256
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(t, name: str, shape, dtype, device) -> int:
+    """Checks a matrix whose rows are contiguous; the distance between rows, in elements."""
+    _need(t.dim() == 2 and tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
+    _need(t.dtype == dtype and t.device == device, f"{name}: {t.dtype} on {t.device}, not {dtype} on {device}")
+    _need(shape[1] == 1 or t.numel() == 0 or t.stride(1) == 1, f"{name}: the values of a row have to be contiguous")
+    return t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _vector(t, name: str, shape, dtype, device) -> int:
+    """Checks a contiguous array; its address, 0 for None."""
+    if t is None:
+        return 0
+    _need(tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
+    _need(t.dtype == dtype and t.device == device, f"{name}: {t.dtype} on {t.device}, not {dtype} on {device}")
+    _need(t.is_contiguous(), f"{name} has to be contiguous")
+    return t.data_ptr()
+
+
+def _output_layer(weight, bias=None) -> wind_output_t:
+    import torch
+    _need(weight.dim() == 2 and weight.dtype in (torch.bfloat16, torch.float32), "weight: a matrix [n_out, H], bf16 or fp32")
+    n_out, H = weight.shape
+    ldw = _rows(weight, "weight", (n_out, H), weight.dtype, weight.device)
+    return wind_output_t(n_out=n_out, H=H, dtype=WIND_DT_BF16 if weight.dtype == torch.bfloat16 else WIND_DT_F32, reserved=0,
+                         w=weight.data_ptr(), ldw=ldw, b=_vector(bias, "bias", (n_out,), torch.float32, weight.device) or None)
+
+
+def wind_loss_workspace_bytes(weight, N: int, K: int = 0, grad: bool = False) -> int:
+    """Workspace of a loss call (grad=True: of a gradient call) for up to N rows, K teacher's entries a row (0: labels)."""
+    o, n = _output_layer(weight), C.c_size_t(0)
+    st = load_library().wind_loss_workspace_bytes(C.byref(o), N, K, int(bool(grad)), C.byref(n))
+    if st != WIND_OK:
+        raise WindError(st)
+    return int(n.value)
+
+
+def alloc_loss_workspace(weight, N: int, K: int = 0, grad: bool = False):
+    """A workspace for loss calls, with grad=True also for gradient calls, of up to N rows."""
+    torch = _torch()
+    n = wind_loss_workspace_bytes(weight, N, K, False)
+    if grad:
+        n = max(n, wind_loss_workspace_bytes(weight, N, K, True))
+    return torch.empty(n + 256, dtype=torch.uint8, device=weight.device)
+
+
+def _loss_call(name: str, x, weight, bias, rows, forward, backward, workspace, stream, check: bool) -> int:
+    """rows: (target,) or (ids, teacher, tau); forward: (loss, lse) or None; backward: (lse, dloss, dx, dw, db) or None."""
+    torch = _torch()
+    o = _output_layer(weight, bias)
+    dev, dt, f32, i32 = weight.device, weight.dtype, torch.float32, torch.int32
+    _need(dev.type == "cuda", "weight: on a CUDA device")
+    _need(x.dim() == 2, "x: a matrix [N, H]")
+    N, H, n_out = x.shape[0], o.H, o.n_out
+    args = [C.byref(o), x.data_ptr(), _rows(x, "x", (N, H), dt, dev)]
+    if len(rows) == 1:
+        args += [_vector(rows[0], "target", (N,), i32, dev), N]
+    else:
+        ids, teacher, tau = rows
+        _need(ids.dim() == 2, "ids: a matrix [N, K]")
+        K = ids.shape[1]
+        args += [_vector(ids, "ids", (N, K), i32, dev), _vector(teacher, "teacher", (N, K), f32, dev), N, K, float(tau)]
+    if forward:
+        args += [_vector(forward[0], "loss", (N,), f32, dev), _vector(forward[1], "lse", (N,), f32, dev)]
+    else:
+        lse, dloss, dx, dw, db = backward
+        args += [_vector(lse, "lse", (N,), f32, dev), _vector(dloss, "dloss", (N,), f32, dev)]
+        for t, n, shape in ((dx, "dx", (N, H)), (dw, "dw", (n_out, H))):
+            args += [0, 0] if t is None else [t.data_ptr(), _rows(t, n, shape, dt, dev)]
+        args += [_vector(db, "db", (n_out,), f32, dev)]
+    _need(workspace.device == dev, f"workspace: on {workspace.device}, not {dev}")
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    _need(stream.device == dev, f"stream: on {stream.device}, not {dev}")
+    args += [_ws_ptr(workspace), _ws_bytes(workspace), int(stream.cuda_stream)]
+    L = load_library()
+    if torch.cuda.current_device() == dev.index:
+        st = getattr(L, name)(*args)
+    else:
+        with torch.cuda.device(dev):
+            st = getattr(L, name)(*args)
+    if st != WIND_OK:
+        raise WindError(st)
+    return wind_loss_status(workspace, stream) if check else st
+
+
+def wind_label_loss(x, weight, bias, target, loss, lse, workspace, stream=None, check: bool = False) -> int:
+    """Cross entropy of the output layer's labels, without keeping the logits.
+
+    x [N, H] and weight [n_out, H] of one dtype (bf16, fp32), rows any distance apart; bias [n_out] fp32 or None; target [N] int32,
+    -1 for rows of padding; loss, lse [N] fp32 are written.  The call only enqueues work; check=True waits for it and raises
+    WindError where a target is no label.
+    """
+    return _loss_call("wind_label_loss", x, weight, bias, (target,), (loss, lse), None, workspace, stream, check)
+
+
+def wind_label_loss_grad(x, weight, bias, target, lse, dloss, dx, dw, db, workspace, stream=None, check: bool = False) -> int:
+    """Gradients of sum(dloss * loss) into dx, dw (of x's dtype) and db (fp32); None: not asked for.  dloss None: ones."""
+    return _loss_call("wind_label_loss_grad", x, weight, bias, (target,), None, (lse, dloss, dx, dw, db), workspace, stream, check)
+
+
+def wind_distill_loss(x, weight, bias, ids, teacher, tau: float, loss, lse, workspace, stream=None, check: bool = False) -> int:
+    """Distillation from a teacher's best labels: ids [N, K] int32 (-1: no entry), teacher [N, K] fp32 logits or log-probabilities."""
+    return _loss_call("wind_distill_loss", x, weight, bias, (ids, teacher, tau), (loss, lse), None, workspace, stream, check)
+
+
+def wind_distill_loss_grad(x, weight, bias, ids, teacher, tau: float, lse, dloss, dx, dw, db, workspace, stream=None, check: bool = False) -> int:
+    """The gradients of wind_distill_loss, as wind_label_loss_grad."""
+    return _loss_call("wind_distill_loss_grad", x, weight, bias, (ids, teacher, tau), None, (lse, dloss, dx, dw, db), workspace, stream, check)
+
+
+def wind_loss_status(workspace, stream=None, check: bool = True) -> int:
+    """Waits for the stream; the status of the last loss or gradient call that used `workspace`."""
+    torch = _torch()
+    if stream is None:
+        stream = torch.cuda.current_stream(workspace.device)
+    with torch.cuda.device(workspace.device):
+        st = load_library().wind_loss_status(_ws_ptr(workspace), int(stream.cuda_stream))
+    if check and st != WIND_OK:
+        raise WindError(st)
+    return st
 
 
 # ---------------------------------------------------------------------------

@@ -3,6 +3,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -11,6 +12,7 @@
 
 #include "wind_internal.cuh"
 #include "wind_loop.cuh"
+#include "wind_loss.cuh"
 
 namespace wind {
 
@@ -469,6 +471,87 @@ wind_status_t wind_window_first_output(const wind_model_t* m, const void* enc, c
     if (s != WIND_OK) return s;
     WIND_CUDA(launch_first_output(logp, enc_len, t0, B, W, m->V + 1, m->blank_id, K, top_label, top_jump, top_logp, (cudaStream_t)stream));
     return read_status(c);
+}
+
+// ---------------------------------------------------------------------------
+// losses of the output layer
+// ---------------------------------------------------------------------------
+static wind_status_t check_output(const wind_output_t* o, int N, int K) {
+    if (!o || o->n_out < 1 || o->H < 1 || o->ldw < 0 || N < 0 || K < 0) return WIND_ERR_INVALID_ARG;
+    if (o->dtype != WIND_DT_F32 && o->dtype != WIND_DT_BF16) return WIND_ERR_INVALID_ARG;
+    if (o->n_out > kLossMaxOut || o->H > kLossMaxH || N > kLossMaxRows || K > kLossMaxK) return WIND_ERR_UNSUPPORTED;
+    return WIND_OK;
+}
+
+wind_status_t wind_loss_workspace_bytes(const wind_output_t* o, int32_t N, int32_t K, int32_t grad, size_t* bytes) {
+    wind_status_t s = check_output(o, N, K);
+    if (s != WIND_OK) return s;
+    if (!bytes) return WIND_ERR_INVALID_ARG;
+    *bytes = loss_layout(*o, N, K, grad != 0).total;
+    return WIND_OK;
+}
+
+// What the four calls have in common; the call's own pointers are set already.
+static wind_status_t enqueue_loss(LossCall& c, const wind_output_t* o, const void* x, int64_t ldx, int N, int K, float tau, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+    wind_status_t s = check_output(o, N, K);
+    if (s != WIND_OK) return s;
+    if (!o->w || !workspace || ldx < 0 || !(tau > 0.f) || !(tau < INFINITY)) return WIND_ERR_INVALID_ARG;
+    if (N > 0 && !x) return WIND_ERR_INVALID_ARG;
+    if (c.grad && ((c.dx && c.lddx < o->H) || (c.dw && c.lddw < o->H))) return WIND_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(workspace) % kAlign) return WIND_ERR_WORKSPACE;
+    c.o = *o;
+    c.x = x; c.ldx = ldx; c.N = N; c.K = K; c.tau = tau;
+    c.lay = loss_layout(*o, N, K, c.grad);
+    if (workspace_bytes < c.lay.total) return WIND_ERR_WORKSPACE;
+    c.ws = static_cast<uint8_t*>(workspace);
+    c.stream = (cudaStream_t)stream;
+    WIND_CUDA(loss_run(c));
+    return WIND_OK;
+}
+
+wind_status_t wind_label_loss(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* target, int32_t N, float* loss, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    if (N > 0 && (!target || !loss || !lse)) return WIND_ERR_INVALID_ARG;
+    LossCall c{};
+    c.target = target; c.loss = loss; c.lse_out = lse;
+    return enqueue_loss(c, o, x, ldx, N, 0, 1.f, workspace, workspace_bytes, stream);
+}
+
+wind_status_t wind_label_loss_grad(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* target, int32_t N, const float* lse,
+                                   const float* dloss, void* dx, int64_t lddx, void* dw, int64_t lddw, float* db, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    if (N > 0 && (!target || !lse)) return WIND_ERR_INVALID_ARG;
+    LossCall c{};
+    c.target = target; c.lse = lse; c.dloss = dloss; c.grad = 1;
+    c.dx = dx; c.lddx = lddx; c.dw = dw; c.lddw = lddw; c.db = db;
+    return enqueue_loss(c, o, x, ldx, N, 0, 1.f, workspace, workspace_bytes, stream);
+}
+
+wind_status_t wind_distill_loss(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* ids, const float* teacher, int32_t N, int32_t K,
+                                float tau, float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (K < 1 || (N > 0 && (!ids || !teacher || !loss || !lse))) return WIND_ERR_INVALID_ARG;
+    LossCall c{};
+    c.ids = ids; c.y = teacher; c.loss = loss; c.lse_out = lse;
+    return enqueue_loss(c, o, x, ldx, N, K, tau, workspace, workspace_bytes, stream);
+}
+
+wind_status_t wind_distill_loss_grad(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* ids, const float* teacher, int32_t N,
+                                     int32_t K, float tau, const float* lse, const float* dloss, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                                     float* db, void* workspace, size_t workspace_bytes, void* stream) {
+    if (K < 1 || (N > 0 && (!ids || !teacher || !lse))) return WIND_ERR_INVALID_ARG;
+    LossCall c{};
+    c.ids = ids; c.y = teacher; c.lse = lse; c.dloss = dloss; c.grad = 1;
+    c.dx = dx; c.lddx = lddx; c.dw = dw; c.lddw = lddw; c.db = db;
+    return enqueue_loss(c, o, x, ldx, N, K, tau, workspace, workspace_bytes, stream);
+}
+
+wind_status_t wind_loss_status(const void* workspace, void* stream) {
+    if (!workspace) return WIND_ERR_INVALID_ARG;
+    LossCtrl h{};
+    WIND_CUDA(cudaMemcpyAsync(&h, workspace, sizeof(h), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
+    WIND_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
+    return (wind_status_t)h.status;
 }
 
 // Scratch of wind_eval_joint_window_static.  In host code `g_static_ws` is only a handle for

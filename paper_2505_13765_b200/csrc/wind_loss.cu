@@ -1,0 +1,1089 @@
+// Losses of the output layer z = W x + b over many rows x, without keeping the logits (sm_100a):
+//
+//     labels    loss_r = lse_v(z_rv) - z_r,t(r)
+//     distill   loss_r = tau^2 sum_k q_rk (ln q_rk - ln p_r,i(r,k)),  q_r = softmax_k(y_rk / tau),  p_r = softmax_v(z_rv / tau)
+//     gradient  g_rv = s_r (p_rv - [sum of q_rk with i(r,k) = v]),  dx = g W,  dW = g^T x,  db = sum_r g_r
+//               (labels: q is one entry of weight 1, tau = 1; s_r is the loss's weight, times tau)
+//
+// Both losses are one computation: a softmax over all outputs against a target distribution of K >= 1 entries.
+//
+//     loss_mark     which rows count; the teacher's entries of a row to probabilities, sorted by label
+//     loss_gather   rows that count, one behind the other, as tensor-core operands: padding costs nothing from here on
+//     loss_pack     W as tensor-core operands, where it is not one already
+//     loss_gemm     FORWARD   128 x 256 tiles of logits on the tensor cores; of each tile's row only (maximum, sum of exponentials,
+//                             sum of q z) leave the chip
+//                   LOGITS    the same tiles again, turned into g, for a piece of the outputs
+//                   PRODUCTS  dx += g W and dW = g^T x of that piece, g as both operands' layouts need it: rows are contiguous along
+//                             the outputs, which is K of the first product and M of the second (the matrix descriptors take either)
+//     loss_combine  a row's partial results to its loss and log-sum-exp
+//     loss_sum      partial sums of dx / dW, where a product is cut along its K to fill the chip; loss_bias: db
+//
+// fp32 operands are cut into three bf16 parts, x = x1 + x2 + x3 with 8 bits each, and a product into the six of nine part products
+// that are not below 2^-24 of it: x1 w1 + (x1 w2 + x2 w1) + (x1 w3 + x2 w2 + x3 w1), smallest first, in one fp32 accumulator.
+// That is fp32 arithmetic at a sixth of the bf16 rate, three times the rate of the fp32 units.
+//
+// Rounding: logits, exponentials, sums and db stay in fp32.  g is rounded to bf16 (three parts of it for fp32 models) because it is a
+// tensor-core operand; dx and dW are accumulated in fp32 and rounded once.
+//
+// Every wait on an mbarrier is bounded: after about two seconds the CTA flags WIND_ERR_TIMEOUT, frees its tensor memory and returns.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <math_constants.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "wind_internal.cuh"
+#include "wind_loop.cuh"
+#include "wind_loss.cuh"
+#include "wind_ptx.cuh"
+
+namespace wind {
+
+// ---------------------------------------------------------------------------
+// sizes
+// ---------------------------------------------------------------------------
+constexpr int LT_N = 256;                 // columns of an output tile (BM = 128 rows)
+constexpr int LT_STAGES = 4;
+constexpr uint32_t LT_STAGE_BYTES = A_STAGE_BYTES + LT_N * BK * 2;
+constexpr int LT_THREADS = 64 + 256;      // warp 0: TMA, warp 1: MMA + tensor memory, warps 2..9: epilogue
+constexpr int LT_BAND = 16;               // row tiles that are worked on together (see tile_of)
+constexpr int ROWS_PER_BLOCK = 64;        // loss_mark, loss_gather
+constexpr int PANEL_BYTES = 64 * BK * 2;  // 64 x 64 bf16
+constexpr int kFillCtas = 148;            // CTAs that a product is cut for
+
+static inline int up(long long a, int b) { return (int)((a + b - 1) / b * b); }
+static inline int cdiv(long long a, int b) { return (int)((a + b - 1) / b); }
+
+LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad) {
+    LossLayout L{};
+    const bool f32 = o.dtype == WIND_DT_F32;
+    L.planes = f32 ? 3 : 1;
+    L.pack_w = f32 || o.H % 8 || o.ldw % 8 || (o.n_out > 1 && o.ldw < o.H) || reinterpret_cast<uintptr_t>(o.w) % 16;
+    L.Hp = up(o.H, 64);
+    L.Npad = up(N, 128);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t at = off; off = align_up(off + bytes); return at; };
+    L.ctrl = take(sizeof(LossCtrl));
+    const size_t np = (size_t)L.Npad;
+    L.counts = take(4 * (size_t)cdiv(N, ROWS_PER_BLOCK));
+    L.mark = take(np);
+    L.src = take(4 * np);
+    L.target = take(K ? 0 : 4 * np);
+    L.scale = take(grad ? 4 * np : 0);
+    L.nlse = take(grad ? 4 * np : 0);
+    L.sid = take(4 * (size_t)N * K);
+    L.sq = take(4 * (size_t)N * K);
+    L.ent = take(K ? 4 * np : 0);
+    L.x = take(2 * (size_t)L.planes * np * L.Hp);
+    L.w = take(L.pack_w ? 2 * (size_t)L.planes * o.n_out * L.Hp : 0);
+    if (!grad) {
+        const size_t parts = (size_t)cdiv(o.n_out, 128);
+        L.pm = take(4 * parts * np);
+        L.ps = take(4 * parts * np);
+        L.pq = take(4 * parts * np);
+    } else {
+        // a piece: as many outputs as keep its g within kLossPieceBytes, 2048 at least (below that the partial sums of dx, read and
+        // written once a piece, cost more than a few per cent of the products)
+        const long long all = up(o.n_out, LT_N);
+        const long long fit = (long long)(kLossPieceBytes / (2 * (size_t)L.planes * (np ? np : 1))) / LT_N * LT_N;
+        L.piece = (int)std::min(all, std::max(2048LL, fit));
+        L.pieces = cdiv(o.n_out, L.piece);
+        const int ht = cdiv(o.H, LT_N), terms = f32 ? 6 : 1;
+        const long long t_dx = (long long)(L.Npad / 128) * ht, t_dw = (long long)cdiv(std::min(o.n_out, L.piece), 128) * ht;
+        const int kb_dx = cdiv(std::min(o.n_out, L.piece), BK), kb_dw = L.Npad / BK;
+        auto parts_of = [&](long long tiles, int kb) {
+            if (tiles <= 0 || tiles >= kFillCtas) return 1;
+            return (int)std::max(1LL, std::min<long long>({kFillCtas / tiles, (long long)kb * terms / 8, (long long)kb}));
+        };
+        L.s_dx = parts_of(t_dx, kb_dx);
+        L.s_dw = parts_of(t_dw, kb_dw);
+        L.slab_dx = L.s_dx > 1 || L.pieces > 1;
+        L.slab_dw = L.s_dw > 1;
+        L.g = take(2 * (size_t)L.planes * np * L.piece);
+        L.dbp = take(4 * (np / 128) * L.piece);
+        L.sdx = take(L.slab_dx ? 4 * (size_t)L.s_dx * np * L.Hp : 0);
+        L.sdw = take(L.slab_dw ? 4 * (size_t)L.s_dw * L.piece * L.Hp : 0);
+    }
+    L.total = off;
+    return L;
+}
+
+// ---------------------------------------------------------------------------
+// rows: which count, and their operands
+// ---------------------------------------------------------------------------
+enum Mark : uint8_t { ROW_NONE = 0, ROW_COUNTS = 1, ROW_BAD = 2 };   // BAD: a label outside [-1, n_out)
+
+struct RowsParams {
+    LossCtrl* ctrl;
+    int N, n_out, K, H, Hp, Npad, x_vec, grad;
+    float tau;
+    const int32_t* target; const int32_t* ids; const float* y;
+    const void* x; int64_t ldx;
+    int32_t* counts; uint8_t* mark; int32_t* src; int32_t* target_c; float* scale_c; float* nlse_c; int32_t* sid; float* sq; float* ent;
+    __nv_bfloat16* xc;
+    float* loss; float* lse_out;
+    const float* lse; const float* dloss;
+    void* dx; int64_t lddx;
+};
+
+// Warp w of a block takes rows w, w + 8, ...  Teacher's lists: probabilities over the entries that are there, and the entries by
+// rising label (equal labels in their order), so that the epilogues walk a list along their columns.  The place of an entry is the
+// number of entries before it: K^2 / 32 comparisons a lane, two per cent of the row's logits at the shapes this is for.
+__global__ void __launch_bounds__(256) loss_mark_kernel(const RowsParams p) {
+    __shared__ int32_t s_ids[8][kLossMaxK];
+    __shared__ int s_count;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int r0 = blockIdx.x * ROWS_PER_BLOCK;
+    if (threadIdx.x == 0) {
+        s_count = 0;
+        if (blockIdx.x == 0) { p.ctrl->status = WIND_OK; p.ctrl->n_rows = 0; }
+    }
+    __syncthreads();
+    if (p.K == 0) {
+        if (threadIdx.x < ROWS_PER_BLOCK && r0 + (int)threadIdx.x < p.N) {
+            const int t = p.target[r0 + threadIdx.x];
+            const uint8_t m = t == -1 ? ROW_NONE : (t >= 0 && t < p.n_out ? ROW_COUNTS : ROW_BAD);
+            p.mark[r0 + threadIdx.x] = m;
+            if (m == ROW_COUNTS) atomicAdd(&s_count, 1);
+        }
+    } else {
+        int32_t* list = s_ids[warp];
+        for (int r = r0 + warp; r < min(r0 + ROWS_PER_BLOCK, p.N); r += 8) {
+            const int32_t* ids = p.ids + (size_t)r * p.K;
+            const float* y = p.y + (size_t)r * p.K;
+            float top = -CUDART_INF_F;
+            int flags = 0;   // 1: an entry outside the outputs, 2: NaN
+            __syncwarp();
+            for (int k = lane; k < p.K; k += 32) {
+                const int id = ids[k];
+                const float v = y[k];
+                if (id < -1 || id >= p.n_out) flags |= 1;
+                const bool there = id >= 0 && id < p.n_out;
+                if (there && v != v) flags |= 2;
+                if (there) top = fmaxf(top, v);
+                list[k] = there ? id : 0x7fffffff;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                flags |= __shfl_xor_sync(0xffffffffu, flags, o);
+            }
+            __syncwarp();
+            float sum = 0.f;
+            for (int k = lane; k < p.K; k += 32)
+                if (list[k] != 0x7fffffff && y[k] != -CUDART_INF_F) sum += expf((y[k] - top) / p.tau);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            const float log_sum = logf(sum);
+            float ent = 0.f;
+            for (int k = lane; k < p.K; k += 32) {
+                const int id = list[k];
+                float q = 0.f;
+                if (id != 0x7fffffff && y[k] != -CUDART_INF_F) {
+                    const float d = (y[k] - top) / p.tau;
+                    q = expf(d) / sum;
+                    if (q != 0.f) ent += q * (d - log_sum);
+                }
+                int place = 0;
+                for (int j = 0; j < p.K; ++j) place += list[j] < id || (list[j] == id && j < k);
+                p.sid[(size_t)r * p.K + place] = id;
+                p.sq[(size_t)r * p.K + place] = q;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) ent += __shfl_xor_sync(0xffffffffu, ent, o);
+            if (lane == 0) {
+                const uint8_t m = (flags & 1) ? ROW_BAD : ((flags & 2) || top != -CUDART_INF_F ? ROW_COUNTS : ROW_NONE);
+                p.mark[r] = m;
+                p.ent[r] = ent;
+                if (m == ROW_COUNTS) atomicAdd(&s_count, 1);
+            }
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) p.counts[blockIdx.x] = s_count;
+}
+
+// Eight columns of a row as fp32; columns from H on are zero.
+template <bool F32>
+__device__ __forceinline__ void load8(const void* row, int c, int H, bool vec, float* v) {
+    if (vec && c + 8 <= H) {
+        if (F32) {
+            const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(row) + c);
+            const float4 a = s[0], b = s[1];
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(row) + c);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = c + i < H ? (F32 ? static_cast<const float*>(row)[c + i] : __bfloat162float(static_cast<const __nv_bfloat16*>(row)[c + i])) : 0.f;
+}
+
+// x = p1 + p2 + p3 with eight bits each (nearest; downwards where nearest would overflow).  Infinities and NaN stand in p1 alone.
+__device__ __forceinline__ void split3(float x, float* part) {
+    float a = __bfloat162float(__float2bfloat16_rn(x));
+    if (isinf(a) && !isinf(x)) a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    const float r = isfinite(a) ? x - a : 0.f;
+    const float b = __bfloat162float(__float2bfloat16_rn(r));
+    part[0] = a; part[1] = b; part[2] = r - b;
+}
+
+template <bool F32>
+__device__ __forceinline__ void store8(__nv_bfloat16* dst, size_t plane, const float* v) {
+    if constexpr (!F32) {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    } else {
+        float s[8][3];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) split3(v[i], s[i]);
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+            *reinterpret_cast<uint4*>(dst + t * plane) = make_uint4(pack_bf16x2(s[0][t], s[1][t]), pack_bf16x2(s[2][t], s[3][t]),
+                                                                    pack_bf16x2(s[4][t], s[5][t]), pack_bf16x2(s[6][t], s[7][t]));
+    }
+}
+
+template <bool F32>
+__device__ __forceinline__ void store_one(void* row, int c, float v) {
+    if (F32) static_cast<float*>(row)[c] = v;
+    else static_cast<__nv_bfloat16*>(row)[c] = __float2bfloat16_rn(v);
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
+    __shared__ int s_warp[8], s_pos[ROWS_PER_BLOCK], s_total;
+    __shared__ uint8_t s_mark[ROWS_PER_BLOCK];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int r0 = blockIdx.x * ROWS_PER_BLOCK;
+    int before = 0;
+    for (int i = threadIdx.x; i < (int)blockIdx.x; i += 256) before += p.counts[i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+    if (lane == 0) s_warp[warp] = before;
+    if (threadIdx.x < ROWS_PER_BLOCK) s_mark[threadIdx.x] = r0 + (int)threadIdx.x < p.N ? p.mark[r0 + threadIdx.x] : (uint8_t)ROW_NONE;
+    __syncthreads();
+    if (warp == 0) {
+        int base = lane < 8 ? s_warp[lane] : 0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) base += __shfl_xor_sync(0xffffffffu, base, o);
+        const uint32_t lo = __ballot_sync(0xffffffffu, s_mark[lane] == ROW_COUNTS), hi = __ballot_sync(0xffffffffu, s_mark[lane + 32] == ROW_COUNTS);
+        const uint32_t bad = __ballot_sync(0xffffffffu, s_mark[lane] == ROW_BAD || s_mark[lane + 32] == ROW_BAD);
+        const uint32_t below = (1u << lane) - 1u;
+        s_pos[lane] = base + __popc(lo & below);
+        s_pos[lane + 32] = base + __popc(lo) + __popc(hi & below);
+        if (lane == 0) {
+            s_total = base + __popc(lo) + __popc(hi);
+            if (bad) atomicCAS(&p.ctrl->status, 0, (int)WIND_ERR_INVALID_ARG);
+        }
+    }
+    __syncthreads();
+    const size_t plane = (size_t)p.Npad * p.Hp;
+    const size_t es = F32 ? 4 : 2;
+    for (int i = warp; i < ROWS_PER_BLOCK && r0 + i < p.N; i += 8) {
+        const int r = r0 + i;
+        if (s_mark[i] == ROW_COUNTS) {
+            const int j = s_pos[i];
+            if (lane == 0) {
+                p.src[j] = r;
+                if (p.K == 0) p.target_c[j] = p.target[r];
+                if (p.grad) {
+                    p.scale_c[j] = (p.dloss ? p.dloss[r] : 1.f) * p.tau;
+                    p.nlse_c[j] = p.lse[r];
+                }
+            }
+            const uint8_t* row = static_cast<const uint8_t*>(p.x) + (size_t)r * p.ldx * es;
+            for (int c = lane * 8; c < p.Hp; c += 256) {
+                float v[8];
+                load8<F32>(row, c, p.H, p.x_vec, v);
+                store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, v);
+            }
+        } else {
+            const float fill = s_mark[i] == ROW_BAD ? CUDART_NAN_F : 0.f;
+            if (!p.grad) {
+                if (lane == 0) { p.loss[r] = fill; p.lse_out[r] = fill; }
+            } else if (p.dx) {
+                uint8_t* row = static_cast<uint8_t*>(p.dx) + (size_t)r * p.lddx * es;
+                for (int c = lane; c < p.H; c += 32) store_one<F32>(row, c, fill);
+            }
+        }
+    }
+    if (blockIdx.x == gridDim.x - 1) {
+        // the last row tile is full of zeros behind the last row
+        const int n = s_total;
+        if (threadIdx.x == 0) p.ctrl->n_rows = n;
+        const float zero[8] = {};
+        for (int j = n + warp; j < (n + 127) / 128 * 128; j += 8)
+            for (int c = lane * 8; c < p.Hp; c += 256) store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, zero);
+    }
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(256) loss_pack_kernel(const void* w, int64_t ldw, int rows, int H, int Hp, int vec, __nv_bfloat16* out) {
+    const size_t plane = (size_t)rows * Hp;
+    const int per_row = Hp / 8;
+    const long long all = (long long)rows * per_row;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+        const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * 8;
+        float v[8];
+        load8<F32>(static_cast<const uint8_t*>(w) + (size_t)r * ldw * (F32 ? 4 : 2), c, H, vec, v);
+        store8<F32>(out + (size_t)r * Hp + c, plane, v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The products: a persistent tcgen05 GEMM with three epilogues
+// ---------------------------------------------------------------------------
+enum LossMode { FORWARD = 0, LOGITS = 1, PRODUCTS = 2 };
+
+struct LossGemm {
+    LossCtrl* ctrl;
+    int n_out, H, Hp, Npad, K;
+    int kb;                       // K blocks of the logits
+    int v0, cols, n_vt;           // this piece's first output, its outputs (to n_out at most) and 256-column tiles
+    float rtau;                   // 1 / tau
+    const float* bias;
+    const int32_t* src; const int32_t* target; const int32_t* sid; const float* sq;
+    float *pm, *ps, *pq;          // FORWARD: [parts][Npad]
+    const float* scale; const float* nlse;
+    __nv_bfloat16* g; int ldg; size_t g_plane; float* dbp;   // LOGITS
+    // PRODUCTS
+    int ht, s_dx, s_dw, add_dx;   // 256-column tiles of H, parts of the sums, whether dx's partial sums are added to
+    float *sdx, *sdw; int slab_rows_dw;   // partial sums, or null: straight to dx / dw
+    void* dx; int64_t lddx; int dx_vec; int want_dx;
+    void* dw; int64_t lddw; int dw_vec; int want_dw;
+};
+
+// Operand parts of the six products of fp32 models, smallest first (bf16 models: the last one alone).
+__device__ __forceinline__ int term_a(int t) { return (0x001102 >> (4 * t)) & 3; }   // 2 0 1 1 0 0
+__device__ __forceinline__ int term_b(int t) { return (0x010120 >> (4 * t)) & 3; }   // 0 2 1 0 1 0
+
+// K-major tiles as in smem_desc_sw128.  MN-major ones: panels of 64 (M or N) x 64 (K) bf16, a K row of a panel being 128 bytes: 8 K rows
+// are a swizzle atom of 1024 bytes (stride byte offset), panels stand PANEL_BYTES apart (leading byte offset).
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t smem_addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(PANEL_BYTES >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+        "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float pick32(const float* v, int at) {
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x = at == i ? v[i] : x;
+    return x;
+}
+
+// What a CTA's roles need to know about a piece of work.
+struct Unit {
+    int mt, nt;          // row tile of A, column tile of B
+    int k0, nk;          // K blocks
+    int dw;              // PRODUCTS: dW (else dx)
+    int part;            // PRODUCTS: which part of the sum
+};
+
+template <int MODE>
+__device__ __forceinline__ long long count_units(const LossGemm& p, int n_rows) {
+    const int mtc = (n_rows + BM - 1) / BM;
+    if (MODE != PRODUCTS) return (long long)mtc * p.n_vt;
+    long long n = 0;
+    if (p.want_dx) n += (long long)p.s_dx * mtc * p.ht;
+    if (p.want_dw) n += (long long)p.s_dw * ((p.cols + BM - 1) / BM) * p.ht;
+    return n;
+}
+
+// Logits: bands of LT_BAND row tiles, in a band row tile fastest, so that the CTAs at work share few tiles of x and of W.
+template <int MODE>
+__device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long u) {
+    Unit t{};
+    const int mtc = (n_rows + BM - 1) / BM;
+    if (MODE != PRODUCTS) {
+        const long long per_band = (long long)LT_BAND * p.n_vt;
+        const int band = (int)(u / per_band);
+        const int r = (int)(u - band * per_band), in_band = min(LT_BAND, mtc - band * LT_BAND);
+        t.nt = r / in_band;
+        t.mt = band * LT_BAND + (r - t.nt * in_band);
+        t.nk = p.kb;
+        return t;
+    }
+    const long long n_dx = p.want_dx ? (long long)p.s_dx * mtc * p.ht : 0;
+    t.dw = u >= n_dx;
+    if (t.dw) u -= n_dx;
+    const int tiles = (t.dw ? (p.cols + BM - 1) / BM : mtc) * p.ht;
+    t.part = (int)(u / tiles);
+    const int r = (int)(u - (long long)t.part * tiles);
+    t.mt = r / p.ht;
+    t.nt = r - t.mt * p.ht;
+    const int kb = t.dw ? (n_rows + BK - 1) / BK : p.n_vt * (LT_N / BK), s = t.dw ? p.s_dw : p.s_dx;
+    t.k0 = (int)((long long)kb * t.part / s);
+    t.nk = (int)((long long)kb * (t.part + 1) / s) - t.k0;
+    return t;
+}
+
+template <int MODE>
+__device__ __forceinline__ int unit_cols(const LossGemm& p, const Unit& t) {   // columns of B that are there
+    return min(LT_N, (MODE == PRODUCTS ? p.H : p.cols) - t.nt * LT_N);
+}
+
+// FORWARD epilogue of one row's 128 columns from `col` (an output) on.
+template <bool LIST>
+__device__ __forceinline__ void forward_row(const LossGemm& p, uint32_t taddr, const float* bias, int col, int n_cols, int row, int n_rows, int part) {
+    float m = -CUDART_INF_F, s = 0.f, qz = 0.f;
+    int target = -1, cur = 0, next = 0x7fffffff;
+    const int32_t* sid = nullptr;
+    const float* sq = nullptr;
+    if (row < n_rows) {
+        if (!LIST) target = p.target[row];
+        else {
+            const size_t at = (size_t)p.src[row] * p.K;
+            sid = p.sid + at;
+            sq = p.sq + at;
+            int lo = 0, hi = p.K;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (sid[mid] < col) lo = mid + 1; else hi = mid;
+            }
+            cur = lo;
+            if (cur < p.K) next = sid[cur];
+        }
+    }
+#pragma unroll 1
+    for (int c0 = 0; c0 < n_cols; c0 += 32) {
+        float v[32];
+        __syncwarp();
+        tmem_ld32(taddr + c0, v);
+        float top = -CUDART_INF_F;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            v[i] = (v[i] + bias[c0 + i]) * p.rtau;
+            top = fmaxf(top, v[i]);
+        }
+        if (!LIST) {
+            const int at = target - (col + c0);
+            if (at >= 0 && at < 32) qz = pick32(v, at);
+        } else {
+            while (next < col + c0 + 32) {
+                const float q = sq[cur], z = pick32(v, next - (col + c0));
+                if (q != 0.f) qz += q * z;
+                ++cur;
+                next = cur < p.K ? sid[cur] : 0x7fffffff;
+            }
+        }
+        const float m1 = fmaxf(m, top), base = m1 == -CUDART_INF_F ? 0.f : m1;
+        float add = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) add += exp2_fast((v[i] - base) * kLog2e);
+        s = s * exp2_fast((m - base) * kLog2e) + add;
+        m = m1;
+    }
+    if (row < n_rows) {
+        const size_t at = (size_t)part * p.Npad + row;
+        p.pm[at] = m;
+        p.ps[at] = s;
+        p.pq[at] = qz;
+    }
+}
+
+// Sums over the 32 lanes of 32 values each: lane l gets the sum of value l.
+__device__ __forceinline__ float column_sums(float* v, int lane) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const bool up_half = lane & o;
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+            const float give = up_half ? v[i] : v[i + o], keep = up_half ? v[i + o] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    return v[0];
+}
+
+// LOGITS epilogue of one row's 128 columns: g, and the warp's share of the columns' sums.
+template <bool LIST, int P>
+__device__ __forceinline__ void logits_row(const LossGemm& p, uint32_t taddr, const float* bias, int col, int g_col, int row, int n_rows, float* sums) {
+    const int lane = threadIdx.x & 31;
+    const bool there = row < n_rows;
+    const float scale = there ? p.scale[row] : 0.f, nlse = there ? p.nlse[row] : 0.f;
+    int target = -1, cur = 0, next = 0x7fffffff;
+    const int32_t* sid = nullptr;
+    const float* sq = nullptr;
+    if (there) {
+        if (!LIST) target = p.target[row];
+        else {
+            const size_t at = (size_t)p.src[row] * p.K;
+            sid = p.sid + at;
+            sq = p.sq + at;
+            int lo = 0, hi = p.K;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (sid[mid] < col) lo = mid + 1; else hi = mid;
+            }
+            cur = lo;
+            if (cur < p.K) next = sid[cur];
+        }
+    }
+    __nv_bfloat16* dst = p.g + (size_t)row * p.ldg + g_col;
+#pragma unroll 1
+    for (int c0 = 0; c0 < 128; c0 += 32) {
+        float v[32];
+        __syncwarp();
+        const bool any = there && col + c0 < p.n_out;   // (behind the outputs the accumulator holds what an earlier tile left)
+        tmem_ld32(taddr + c0, v);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = scale * exp2_fast(((v[i] + bias[c0 + i]) * p.rtau - nlse) * kLog2e);
+        if (!LIST) {
+            const int at = target - (col + c0);
+            if (at >= 0 && at < 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = at == i ? v[i] - scale : v[i];
+            }
+        } else {
+            while (next < col + c0 + 32) {
+                const float q = scale * sq[cur];
+                const int at = next - (col + c0);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = at == i ? v[i] - q : v[i];
+                ++cur;
+                next = cur < p.K ? sid[cur] : 0x7fffffff;
+            }
+        }
+        if (!any) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+        }
+        if (P == 1) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) store8<false>(dst + c0 + i, 0, v + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) store8<true>(dst + c0 + i, p.g_plane, v + i);
+        }
+        if (p.dbp) {
+            const float sum = column_sums(v, lane);
+            sums[c0 + lane] = sum;
+        }
+    }
+}
+
+// PRODUCTS epilogue of one row's columns [h, H) that belong to its half of the tile; zero: the sum has no term.
+template <bool F32>
+__device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, uint32_t taddr, int half, int row_in_tile, int n_rows, bool zero) {
+    const int row = t.mt * BM + row_in_tile;                       // of dx: a gathered row; of dW: an output of the piece
+    const bool there = row < (t.dw ? p.cols : n_rows);
+    float* slab = t.dw ? p.sdw : p.sdx;
+    const int h0 = t.nt * LT_N + half * 128, h1 = min(h0 + 128, slab ? p.Hp : p.H);
+    uint8_t* out = nullptr;
+    float* sum = nullptr;
+    if (there) {
+        if (slab) sum = slab + ((size_t)t.part * (t.dw ? p.slab_rows_dw : p.Npad) + row) * p.Hp;
+        else if (t.dw) out = static_cast<uint8_t*>(p.dw) + (size_t)(p.v0 + row) * p.lddw * (F32 ? 4 : 2);
+        else out = static_cast<uint8_t*>(p.dx) + (size_t)p.src[row] * p.lddx * (F32 ? 4 : 2);
+    }
+    const bool vec = t.dw ? p.dw_vec : p.dx_vec;
+#pragma unroll 1
+    for (int h = h0; h < h1; h += 32) {
+        float v[32];
+        __syncwarp();
+        if (zero) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+        } else tmem_ld32(taddr + (h - h0), v);
+        if (!there) {
+        } else if (sum) {
+            float4* d = reinterpret_cast<float4*>(sum + h);
+            const bool add = !t.dw && p.add_dx;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float4 o = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                if (add) { const float4 b = d[i]; o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w; }
+                d[i] = o;
+            }
+        } else if (vec && h + 32 <= h1) {
+            if (F32) {
+                float4* d = reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) store8<false>(reinterpret_cast<__nv_bfloat16*>(out) + h + i, 0, v + i);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (h + i < h1) store_one<F32>(out, h + i, v[i]);
+        }
+    }
+}
+
+template <int MODE, bool LIST, int P>
+__global__ void __launch_bounds__(LT_THREADS, 1)
+loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a2,
+                 const __grid_constant__ CUtensorMap map_b2, const LossGemm p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_bar[LT_STAGES], empty_bar[LT_STAGES], acc_full[2], acc_empty[2], drain_bar;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    __shared__ float s_bias[2][LT_N];
+    __shared__ float s_db[8][128];
+
+    const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
+    uint8_t* smem = align_smem_1024(smem_raw);
+    constexpr int TERMS = P == 3 ? 6 : 1;
+    constexpr int FIRST_TERM = 6 - TERMS;
+
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < LT_STAGES; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], 8); }
+        mbar_init(&drain_bar, 1);
+        fence_barrier_init();
+        prefetch_tmap(&map_a); prefetch_tmap(&map_b);
+        if (MODE == PRODUCTS) { prefetch_tmap(&map_a2); prefetch_tmap(&map_b2); }
+    }
+    if (warp == 1) tmem_alloc(&tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_slot;
+    const int n_rows = p.ctrl->n_rows;
+    const long long n_units = count_units<MODE>(p, n_rows);
+
+    if (warp == 0) {
+        if (elect_one()) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+                const Unit t = unit_of<MODE>(p, n_rows, u);
+                const int panels = (unit_cols<MODE>(p, t) + 63) / 64;
+                for (int term = FIRST_TERM; term < 6 && ok; ++term) {
+                    const int pa = term_a(term), pb = term_b(term);
+                    for (int kb = t.k0; kb < t.k0 + t.nk; ++kb, ++it) {
+                        const int s = it % LT_STAGES;
+                        if (!mbar_wait(&empty_bar[s], ((it / LT_STAGES) & 1) ^ 1, &abort_flag)) { ok = false; break; }
+                        uint8_t* a = smem + (size_t)s * LT_STAGE_BYTES;
+                        uint8_t* b = a + A_STAGE_BYTES;
+                        if (MODE != PRODUCTS) {
+                            mbar_expect_tx(&full_bar[s], LT_STAGE_BYTES);
+                            tma_load_3d(a, &map_a, kb * BK, t.mt * BM, pa, &full_bar[s]);
+                            tma_load_3d(b, &map_b, kb * BK, p.v0 + t.nt * LT_N, pb, &full_bar[s]);
+                        } else {
+                            mbar_expect_tx(&full_bar[s], (uint32_t)(A_STAGE_BYTES + panels * PANEL_BYTES));
+                            if (!t.dw) {
+                                tma_load_3d(a, &map_a, kb * BK, t.mt * BM, pa, &full_bar[s]);
+                                for (int q = 0; q < panels; ++q)
+                                    tma_load_3d(b + q * PANEL_BYTES, &map_b, t.nt * LT_N + q * 64, p.v0 + kb * BK, pb, &full_bar[s]);
+                            } else {
+                                for (int q = 0; q < 2; ++q)
+                                    tma_load_3d(a + q * PANEL_BYTES, &map_a2, t.mt * BM + q * 64, kb * BK, pa, &full_bar[s]);
+                                for (int q = 0; q < panels; ++q)
+                                    tma_load_3d(b + q * PANEL_BYTES, &map_b2, t.nt * LT_N + q * 64, kb * BK, pb, &full_bar[s]);
+                            }
+                        }
+                    }
+                }
+            }
+            if (!ok) {   // given up: the copies in flight still write into this CTA's shared memory
+                int late = 0;
+                for (uint32_t i = it > LT_STAGES ? it - LT_STAGES : 0; i < it; ++i) mbar_wait(&full_bar[i % LT_STAGES], (i / LT_STAGES) & 1, &late);
+            }
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            uint32_t it = 0, n_acc = 0;
+            bool ok = true;
+            for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+                const Unit t = unit_of<MODE>(p, n_rows, u);
+                if (t.nk == 0) continue;
+                const int n = (unit_cols<MODE>(p, t) + 31) / 32 * 32;   // (the epilogues read 32 columns at a time)
+                const bool a_mn = MODE == PRODUCTS && t.dw, b_mn = MODE == PRODUCTS;
+                const uint32_t idesc = idesc_bf16(BM, n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+                const uint64_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;   // 16 of K, in units of 16 bytes
+                const uint32_t acc = n_acc & 1u;
+                if (!mbar_wait(&acc_empty[acc], ((n_acc >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t tm_d = tmem_base + acc * LT_N;
+                const int blocks = t.nk * TERMS;
+                for (int i = 0; i < blocks; ++i, ++it) {
+                    const int s = it % LT_STAGES;
+                    if (!mbar_wait(&full_bar[s], (it / LT_STAGES) & 1, &abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t a_addr = smem_u32(smem + (size_t)s * LT_STAGE_BYTES), b_addr = a_addr + A_STAGE_BYTES;
+                    const uint64_t adesc = a_mn ? smem_desc_mn(a_addr) : smem_desc_sw128(a_addr);
+                    const uint64_t bdesc = b_mn ? smem_desc_mn(b_addr) : smem_desc_sw128(b_addr);
+#pragma unroll
+                    for (int k = 0; k < BK / 16; ++k) tc_mma_bf16(tm_d, adesc + k * a_step, bdesc + k * b_step, idesc, (i | k) != 0);
+                    tc_commit(&empty_bar[s]);
+                }
+                if (ok) tc_commit(&acc_full[acc]);
+                ++n_acc;
+            }
+            if (!ok) {   // given up: the products in flight still read it
+                int late = 0;
+                tc_commit(&drain_bar);
+                mbar_wait(&drain_bar, 0, &late);
+            }
+        }
+    } else {
+        const int q = warp & 3, half = (warp - 2) >> 2;   // tensor-memory lane quadrant; which 128 columns
+        const int et = threadIdx.x - 64;                  // 0..255
+        const int row_in_tile = q * 32 + lane;
+        uint32_t n_acc = 0;
+        bool ok = true;
+        for (long long u = blockIdx.x; u < n_units; u += gridDim.x) {
+            const Unit t = unit_of<MODE>(p, n_rows, u);
+            const uint32_t acc = n_acc & 1u;
+            const uint32_t taddr = tmem_base + acc * LT_N + half * 128 + ((uint32_t)(q * 32) << 16);
+            const int row = t.mt * BM + row_in_tile;
+            if (MODE != PRODUCTS) {
+                const int v = p.v0 + t.nt * LT_N + et;     // outputs behind the last one: probability zero
+                s_bias[acc][et] = v < p.n_out ? (p.bias ? p.bias[v] : 0.f) : -CUDART_INF_F;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            }
+            // (a warp that gives up goes on without waiting: the others still meet it at the barriers)
+            if (t.nk > 0) {
+                ok = ok && mbar_wait_warp(&acc_full[acc], (n_acc >> 1) & 1u, &abort_flag);
+                tc_fence_after();
+            }
+            const int col = p.v0 + t.nt * LT_N + half * 128;
+            if (!ok) {
+            } else if (MODE == FORWARD) {
+                const int n_cols = min(128, p.n_out - col);
+                if (n_cols > 0) forward_row<LIST>(p, taddr, s_bias[acc] + half * 128, col, n_cols, row, n_rows, t.nt * 2 + half);
+            } else if (MODE == LOGITS) {
+                logits_row<LIST, P>(p, taddr, s_bias[acc] + half * 128, col, t.nt * LT_N + half * 128, row, n_rows, s_db[half * 4 + q]);
+            } else {
+                product_row<P == 3>(p, t, taddr, half, row_in_tile, n_rows, t.nk == 0);
+            }
+            if (t.nk > 0) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&acc_empty[acc]);
+                ++n_acc;
+            }
+            if (MODE == LOGITS && p.dbp) {
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                const float* d = &s_db[et >> 7 << 2][et & 127];
+                p.dbp[(size_t)t.mt * p.ldg + t.nt * LT_N + et] = (d[0] + d[128]) + (d[256] + d[384]);
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 512);
+    }
+    if (threadIdx.x == 0 && abort_flag) atomicCAS(&p.ctrl->status, 0, (int)WIND_ERR_TIMEOUT);
+}
+
+// ---------------------------------------------------------------------------
+// what is left
+// ---------------------------------------------------------------------------
+// 32 rows x 8 slices of the partial results a block.
+__global__ void __launch_bounds__(256) loss_combine_kernel(const LossCtrl* ctrl, const int32_t* src, const float* pm, const float* ps, const float* pq,
+                                                           int parts, int Npad, const float* ent, float tau, float* loss, float* lse) {
+    __shared__ float s_m[8][32], s_s[8][32], s_q[8][32];
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    const int j = blockIdx.x * 32 + lane, n = ctrl->n_rows;
+    if ((int)blockIdx.x * 32 >= n) return;
+    float m = -CUDART_INF_F, s = 0.f, qz = 0.f;
+    auto add = [&](float m2, float s2) {
+        const float m1 = fmaxf(m, m2), base = m1 == -CUDART_INF_F ? 0.f : m1;
+        s = s * expf(m - base) + s2 * expf(m2 - base);
+        m = m1;
+    };
+    if (j < n)
+        for (int i = slice; i < parts; i += 8) {
+            const size_t at = (size_t)i * Npad + j;
+            add(pm[at], ps[at]);
+            qz += pq[at];
+        }
+    s_m[slice][lane] = m; s_s[slice][lane] = s; s_q[slice][lane] = qz;
+    __syncthreads();
+    if (slice || j >= n) return;
+    for (int i = 1; i < 8; ++i) {
+        add(s_m[i][lane], s_s[i][lane]);
+        qz += s_q[i][lane];
+    }
+    const int r = src[j];
+    const float log_s = logf(s);
+    // (maximum minus the targets' mean logit first: both are large where the logits are)
+    const float ce = (m - qz) + log_s;
+    loss[r] = ent ? tau * tau * (ent[r] + ce) : ce;
+    lse[r] = m + log_s;
+}
+
+// Partial sums of dx (rows: those that count, to their places) or dW (rows: a piece's outputs).
+template <bool F32>
+__global__ void __launch_bounds__(256) loss_sum_kernel(const LossCtrl* ctrl, const float* slab, int parts, int slab_rows, int rows, int H, int Hp,
+                                                       const int32_t* src, void* out, int64_t ld, int vec) {
+    if (src) rows = ctrl->n_rows;
+    const int per_row = (H + 3) / 4;
+    const long long all = (long long)rows * per_row;
+    const size_t stride = (size_t)slab_rows * Hp;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+        const int r = (int)(i / per_row), h = (int)(i - (long long)r * per_row) * 4;
+        const float* at = slab + (size_t)r * Hp + h;
+        float4 a = *reinterpret_cast<const float4*>(at);
+        for (int k = 1; k < parts; ++k) {
+            const float4 b = *reinterpret_cast<const float4*>(at + k * stride);
+            a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+        }
+        uint8_t* row = static_cast<uint8_t*>(out) + (size_t)(src ? src[r] : r) * ld * (F32 ? 4 : 2);
+        const float v[4] = {a.x, a.y, a.z, a.w};
+        if (vec) {
+            if (F32) reinterpret_cast<float4*>(row)[h / 4] = a;
+            else reinterpret_cast<uint2*>(row)[h / 4] = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (h + k < H) store_one<F32>(row, h + k, v[k]);
+        }
+    }
+}
+
+// db of a piece: sums of the row tiles' column sums, 32 outputs x 8 slices a block.
+__global__ void __launch_bounds__(256) loss_bias_kernel(const LossCtrl* ctrl, const float* dbp, int ld, int cols, float* db) {
+    __shared__ float s_sum[8][32];
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    const int tiles = (ctrl->n_rows + BM - 1) / BM;
+    float sum = 0.f;
+    if (c < cols)
+        for (int i = slice; i < tiles; i += 8) sum += dbp[(size_t)i * ld + c];
+    s_sum[slice][lane] = sum;
+    __syncthreads();
+    if (slice || c >= cols) return;
+    for (int i = 1; i < 8; ++i) sum += s_sum[i][lane];
+    db[c] = sum;
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+static PFN_cuTensorMapEncodeTiled g_encode_loss = nullptr;
+static std::mutex g_loss_mutex;
+
+static cudaError_t get_encode_loss() {
+    std::lock_guard<std::mutex> lock(g_loss_mutex);
+    if (g_encode_loss) return cudaSuccess;
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+    if (e != cudaSuccess) return e;
+    if (q != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
+    g_encode_loss = reinterpret_cast<PFN_cuTensorMapEncodeTiled>(fn);
+    return cudaSuccess;
+}
+
+// bf16 [planes][rows][cols], rows `ld` elements apart, box = 64 columns x box_rows rows, 128-byte swizzle, zero fill outside
+static cudaError_t loss_map(CUtensorMap* map, const void* base, uint64_t planes, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows) {
+    cuuint64_t dims[3] = {cols, rows, planes};
+    cuuint64_t strides[2] = {ld * 2, rows * ld * 2};
+    cuuint32_t box[3] = {(cuuint32_t)BK, box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = g_encode_loss(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+constexpr size_t kLossSmem = (size_t)LT_STAGES * LT_STAGE_BYTES + 1024;
+
+typedef void (*LossKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const LossGemm);
+
+static LossKernel loss_kernel_of(int mode, bool list, int planes) {
+    if (mode == FORWARD) {
+        if (planes == 1) return list ? loss_gemm_kernel<FORWARD, true, 1> : loss_gemm_kernel<FORWARD, false, 1>;
+        return list ? loss_gemm_kernel<FORWARD, true, 3> : loss_gemm_kernel<FORWARD, false, 3>;
+    }
+    if (mode == LOGITS) {
+        if (planes == 1) return list ? loss_gemm_kernel<LOGITS, true, 1> : loss_gemm_kernel<LOGITS, false, 1>;
+        return list ? loss_gemm_kernel<LOGITS, true, 3> : loss_gemm_kernel<LOGITS, false, 3>;
+    }
+    return planes == 1 ? loss_gemm_kernel<PRODUCTS, false, 1> : loss_gemm_kernel<PRODUCTS, false, 3>;
+}
+
+// Shared-memory opt-in of the kernels of this file.
+static cudaError_t loss_set_attributes() {
+    static bool done_on[64] = {};   // the attribute belongs to the (function, device) pair
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(g_loss_mutex);
+    if (done_on[dev]) return cudaSuccess;
+    for (int mode = FORWARD; mode <= PRODUCTS; ++mode)
+        for (int list = 0; list < 2; ++list)
+            for (int planes = 1; planes <= 3; planes += 2)
+                if ((e = cudaFuncSetAttribute(loss_kernel_of(mode, list, planes), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLossSmem)) != cudaSuccess)
+                    return e;
+    done_on[dev] = true;
+    return cudaSuccess;
+}
+
+static bool vec_rows(const void* p, int64_t ld, int H, bool f32) {   // 16-byte accesses of rows of H elements
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % (f32 ? 4 : 8) == 0 && H % 8 == 0;
+}
+
+cudaError_t loss_run(const LossCall& c) {
+    const LossLayout& L = c.lay;
+    const bool f32 = c.o.dtype == WIND_DT_F32;
+    const size_t es = f32 ? 4 : 2;
+    // tensor maps need the device's context in this thread; a stream's flags, which see to that, may not be asked for in a capture
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(c.stream, &capture);
+    if (e == cudaSuccess && capture == cudaStreamCaptureStatusNone) e = bind_context(c.stream);
+    if (e != cudaSuccess) return e;
+    LossCtrl* ctrl = reinterpret_cast<LossCtrl*>(c.ws + L.ctrl);
+    if (c.N == 0) {   // no rows: no loss, no gradient
+        e = cudaMemsetAsync(ctrl, 0, sizeof(LossCtrl), c.stream);
+        if (e == cudaSuccess && c.grad && c.dw) e = cudaMemset2DAsync(c.dw, (size_t)c.lddw * es, 0, (size_t)c.o.H * es, (size_t)c.o.n_out, c.stream);
+        if (e == cudaSuccess && c.grad && c.db) e = cudaMemsetAsync(c.db, 0, 4 * (size_t)c.o.n_out, c.stream);
+        return e;
+    }
+    if ((e = get_encode_loss()) != cudaSuccess) return e;
+    if ((e = loss_set_attributes()) != cudaSuccess) return e;
+    int sms = 0;
+    if ((e = loop_sm_count(&sms)) != cudaSuccess) return e;
+
+    RowsParams r{};
+    r.ctrl = ctrl;
+    r.N = c.N; r.n_out = c.o.n_out; r.K = c.K; r.H = c.o.H; r.Hp = L.Hp; r.Npad = L.Npad; r.grad = c.grad;
+    r.x_vec = vec_rows(c.x, c.ldx, c.o.H, f32);
+    r.tau = c.tau;
+    r.target = c.target; r.ids = c.ids; r.y = c.y; r.x = c.x; r.ldx = c.ldx;
+    r.counts = reinterpret_cast<int32_t*>(c.ws + L.counts);
+    r.mark = c.ws + L.mark;
+    r.src = reinterpret_cast<int32_t*>(c.ws + L.src);
+    r.target_c = reinterpret_cast<int32_t*>(c.ws + L.target);
+    r.scale_c = reinterpret_cast<float*>(c.ws + L.scale);
+    r.nlse_c = reinterpret_cast<float*>(c.ws + L.nlse);
+    r.sid = reinterpret_cast<int32_t*>(c.ws + L.sid);
+    r.sq = reinterpret_cast<float*>(c.ws + L.sq);
+    r.ent = reinterpret_cast<float*>(c.ws + L.ent);
+    r.xc = reinterpret_cast<__nv_bfloat16*>(c.ws + L.x);
+    r.loss = c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.dloss; r.dx = c.dx; r.lddx = c.lddx;
+    const int row_blocks = cdiv(c.N, ROWS_PER_BLOCK);
+    loss_mark_kernel<<<row_blocks, 256, 0, c.stream>>>(r);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (f32) loss_gather_kernel<true><<<row_blocks, 256, 0, c.stream>>>(r);
+    else loss_gather_kernel<false><<<row_blocks, 256, 0, c.stream>>>(r);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+
+    const void* w = c.o.w;
+    int64_t ldw = c.o.ldw;
+    int w_cols = c.o.H;
+    if (L.pack_w) {
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(c.ws + L.w);
+        const int blocks = (int)std::min<long long>(((long long)c.o.n_out * (L.Hp / 8) + 255) / 256, 8LL * sms);
+        const int vec = vec_rows(c.o.w, c.o.ldw, c.o.H, f32);
+        if (f32) loss_pack_kernel<true><<<blocks, 256, 0, c.stream>>>(w, ldw, c.o.n_out, c.o.H, L.Hp, vec, out);
+        else loss_pack_kernel<false><<<blocks, 256, 0, c.stream>>>(w, ldw, c.o.n_out, c.o.H, L.Hp, vec, out);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        w = out; ldw = L.Hp; w_cols = L.Hp;
+    }
+
+    LossGemm p{};
+    p.ctrl = ctrl;
+    p.n_out = c.o.n_out; p.H = c.o.H; p.Hp = L.Hp; p.Npad = L.Npad; p.K = c.K;
+    p.kb = L.Hp / BK;
+    p.rtau = 1.f / c.tau;
+    p.bias = c.o.b;
+    p.src = r.src; p.target = r.target_c; p.sid = r.sid; p.sq = r.sq;
+    CUtensorMap map_x, map_w, map_w64, map_x64, map_g, map_g64;
+    if ((e = loss_map(&map_x, r.xc, L.planes, L.Npad, L.Hp, L.Hp, BM)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_w, w, L.planes, c.o.n_out, w_cols, ldw, LT_N)) != cudaSuccess) return e;
+    const int row_tiles = L.Npad / BM;
+    if (!c.grad) {
+        p.v0 = 0; p.cols = c.o.n_out; p.n_vt = cdiv(c.o.n_out, LT_N);
+        p.pm = reinterpret_cast<float*>(c.ws + L.pm);
+        p.ps = reinterpret_cast<float*>(c.ws + L.ps);
+        p.pq = reinterpret_cast<float*>(c.ws + L.pq);
+        const int grid = (int)std::min<long long>((long long)row_tiles * p.n_vt, sms);
+        loss_kernel_of(FORWARD, c.K > 0, L.planes)<<<grid, LT_THREADS, kLossSmem, c.stream>>>(map_x, map_w, map_x, map_w, p);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        loss_combine_kernel<<<cdiv(c.N, 32), 256, 0, c.stream>>>(ctrl, r.src, p.pm, p.ps, p.pq, cdiv(c.o.n_out, 128), L.Npad,
+                                                                  c.K ? r.ent : nullptr, c.tau, c.loss, c.lse_out);
+        return cudaGetLastError();
+    }
+
+    p.scale = r.scale_c; p.nlse = r.nlse_c;
+    p.g = reinterpret_cast<__nv_bfloat16*>(c.ws + L.g);
+    p.ldg = L.piece; p.g_plane = (size_t)L.Npad * L.piece;
+    p.dbp = c.db ? reinterpret_cast<float*>(c.ws + L.dbp) : nullptr;
+    p.ht = cdiv(c.o.H, LT_N); p.s_dx = L.s_dx; p.s_dw = L.s_dw;
+    p.sdx = L.slab_dx ? reinterpret_cast<float*>(c.ws + L.sdx) : nullptr;
+    p.sdw = L.slab_dw ? reinterpret_cast<float*>(c.ws + L.sdw) : nullptr;
+    p.slab_rows_dw = L.piece;
+    p.dx = c.dx; p.lddx = c.lddx; p.want_dx = c.dx != nullptr; p.dx_vec = vec_rows(c.dx, c.lddx, c.o.H, f32);
+    p.dw = c.dw; p.lddw = c.lddw; p.want_dw = c.dw != nullptr; p.dw_vec = vec_rows(c.dw, c.lddw, c.o.H, f32);
+    if ((e = loss_map(&map_g, p.g, L.planes, L.Npad, L.piece, L.piece, BM)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_g64, p.g, L.planes, L.Npad, L.piece, L.piece, 64)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_x64, r.xc, L.planes, L.Npad, L.Hp, L.Hp, 64)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_w64, w, L.planes, c.o.n_out, w_cols, ldw, 64)) != cudaSuccess) return e;
+    const int sum_blocks = 8 * sms;
+    for (int piece = 0; piece < L.pieces; ++piece) {
+        p.v0 = piece * L.piece;
+        p.cols = std::min(L.piece, c.o.n_out - p.v0);
+        p.n_vt = cdiv(p.cols, LT_N);
+        p.add_dx = piece > 0;
+        int grid = (int)std::min<long long>((long long)row_tiles * p.n_vt, sms);
+        loss_kernel_of(LOGITS, c.K > 0, L.planes)<<<grid, LT_THREADS, kLossSmem, c.stream>>>(map_x, map_w, map_x, map_w, p);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if (c.db) {
+            loss_bias_kernel<<<cdiv(p.cols, 32), 256, 0, c.stream>>>(ctrl, p.dbp, L.piece, p.cols, c.db + p.v0);
+            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        }
+        if (!c.dx && !c.dw) continue;
+        const long long units = (c.dx ? (long long)L.s_dx * row_tiles * p.ht : 0) + (c.dw ? (long long)L.s_dw * cdiv(p.cols, BM) * p.ht : 0);
+        grid = (int)std::min<long long>(units, sms);
+        loss_kernel_of(PRODUCTS, false, L.planes)<<<grid, LT_THREADS, kLossSmem, c.stream>>>(map_g, map_w64, map_g64, map_x64, p);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if (c.dw && L.slab_dw) {
+            void* out = static_cast<uint8_t*>(c.dw) + (size_t)p.v0 * c.lddw * es;
+            if (f32) loss_sum_kernel<true><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdw, L.s_dw, L.piece, p.cols, c.o.H, L.Hp, nullptr, out, c.lddw, p.dw_vec);
+            else loss_sum_kernel<false><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdw, L.s_dw, L.piece, p.cols, c.o.H, L.Hp, nullptr, out, c.lddw, p.dw_vec);
+            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        }
+    }
+    if (c.dx && L.slab_dx) {
+        if (f32) loss_sum_kernel<true><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdx, L.s_dx, L.Npad, 0, c.o.H, L.Hp, r.src, c.dx, c.lddx, p.dx_vec);
+        else loss_sum_kernel<false><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdx, L.s_dx, L.Npad, 0, c.o.H, L.Hp, r.src, c.dx, c.lddx, p.dx_vec);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace wind

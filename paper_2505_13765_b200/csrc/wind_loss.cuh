@@ -1,0 +1,52 @@
+// Losses of the output layer (wind_loss.cu): sizes, workspace layout and the launcher that the entry points call.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "wind.h"
+
+namespace wind {
+
+constexpr int kLossMaxK = 256;            // teacher's entries of a row
+constexpr int kLossMaxRows = 1 << 24;
+constexpr int kLossMaxOut = 1 << 24;
+constexpr int kLossMaxH = 1 << 16;
+constexpr size_t kLossPieceBytes = (size_t)512 << 20;   // the gradient's share of logits that is kept at a time (see loss_layout)
+
+// Control words, first thing in the workspace.
+struct LossCtrl {
+    int32_t status;   // wind_status_t, first error wins
+    int32_t n_rows;   // rows with a loss
+};
+
+// How a call is cut up, and the byte offsets of its workspace regions.  Host arithmetic on the sizes alone.
+struct LossLayout {
+    int planes;        // bf16 parts of an operand: 1 (bf16) or 3 (fp32)
+    int pack_w;        // W is laid out again: fp32, or rows that TMA cannot start on
+    int Hp, Npad;      // H up to a multiple of 64, N up to a multiple of 128
+    int piece;         // outputs of a piece (gradient), a multiple of 256
+    int pieces;
+    int s_dx, s_dw;    // parts that the sums of dx (over a piece's outputs) and dW (over the rows) are cut into
+    int slab_dx, slab_dw;   // whether dx / dW go through fp32 partial sums
+    size_t ctrl, counts, mark, src, target, scale, nlse, sid, sq, ent, x, w, pm, ps, pq, g, dbp, sdx, sdw, total;
+};
+
+struct LossCall {
+    wind_output_t o;
+    const void* x; int64_t ldx; int N;
+    const int32_t* target;                              // labels, or null:
+    const int32_t* ids; const float* y; int K; float tau;   // the teacher's entries
+    float* loss; float* lse_out;                        // forward
+    const float* lse; const float* dloss;               // gradient
+    void* dx; int64_t lddx; void* dw; int64_t lddw; float* db;
+    int grad;
+    uint8_t* ws;
+    LossLayout lay;
+    cudaStream_t stream;
+};
+
+LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad);
+cudaError_t loss_run(const LossCall& c);
+
+}  // namespace wind
