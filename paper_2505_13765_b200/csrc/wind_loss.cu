@@ -7,7 +7,7 @@
 //
 // Both losses are one computation: a softmax over all outputs against a target distribution of K >= 1 entries.
 //
-//     loss_mark     which rows count; the teacher's entries of a row to probabilities, sorted by label
+//     loss_list     the teacher's entries of a row to probabilities, sorted by label
 //     loss_gather   rows that count, one behind the other, as tensor-core operands: padding costs nothing from here on
 //     loss_pack     W as tensor-core operands, where it is not one already
 //     loss_gemm     FORWARD   128 x 256 tiles of logits on the tensor cores; of each tile's row only (maximum, sum of exponentials,
@@ -48,7 +48,7 @@ constexpr int LT_STAGES = 4;
 constexpr uint32_t LT_STAGE_BYTES = A_STAGE_BYTES + LT_N * BK * 2;
 constexpr int LT_THREADS = 64 + 256;      // warp 0: TMA, warp 1: MMA + tensor memory, warps 2..9: epilogue
 constexpr int LT_BAND = 16;               // row tiles that are worked on together (see tile_of)
-constexpr int ROWS_PER_BLOCK = 64;        // loss_mark, loss_gather
+constexpr int ROWS_COUNTED = 8192;        // longer calls have the rows that count counted by a kernel of its own, so many at a time
 constexpr int PANEL_BYTES = 64 * BK * 2;  // 64 x 64 bf16
 constexpr int kFillCtas = 148;            // CTAs that a product is cut for
 
@@ -66,8 +66,8 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad) {
     auto take = [&](size_t bytes) { size_t at = off; off = align_up(off + bytes); return at; };
     L.ctrl = take(sizeof(LossCtrl));
     const size_t np = (size_t)L.Npad;
-    L.counts = take(4 * (size_t)cdiv(N, ROWS_PER_BLOCK));
-    L.mark = take(np);
+    L.counts = take(N > ROWS_COUNTED ? 4 * (size_t)cdiv(N, ROWS_COUNTED) : 0);
+    L.mark = take(K ? np : 0);
     L.src = take(4 * np);
     L.target = take(K ? 0 : 4 * np);
     L.scale = take(grad ? 4 * np : 0);
@@ -117,6 +117,8 @@ enum Mark : uint8_t { ROW_NONE = 0, ROW_COUNTS = 1, ROW_BAD = 2 };   // BAD: a l
 struct RowsParams {
     LossCtrl* ctrl;
     int N, n_out, K, H, Hp, Npad, x_vec, grad;
+    int counted;               // counts[] holds the rows that count, of every ROWS_COUNTED rows
+    int per_block;             // rows of a block of loss_gather, a multiple of 8
     float tau;
     const int32_t* target; const int32_t* ids; const float* y;
     const void* x; int64_t ldx;
@@ -127,79 +129,86 @@ struct RowsParams {
     void* dx; int64_t lddx;
 };
 
-// Warp w of a block takes rows w, w + 8, ...  Teacher's lists: probabilities over the entries that are there, and the entries by
-// rising label (equal labels in their order), so that the epilogues walk a list along their columns.  The place of an entry is the
-// number of entries before it: K^2 / 32 comparisons a lane, two per cent of the row's logits at the shapes this is for.
-__global__ void __launch_bounds__(256) loss_mark_kernel(const RowsParams p) {
+__device__ __forceinline__ uint8_t row_mark(const RowsParams& p, int r) {
+    if (p.K) return p.mark[r];
+    const int t = p.target[r];
+    return t == -1 ? ROW_NONE : (t >= 0 && t < p.n_out ? ROW_COUNTS : ROW_BAD);
+}
+
+// The teacher's list of a row, a warp each: probabilities over the entries that are there, and the entries by rising label (equal
+// labels in their order), so that the epilogues walk a list along their columns.  The place of an entry is the number of entries
+// before it: K^2 / 32 comparisons a lane.
+__global__ void __launch_bounds__(256) loss_list_kernel(const RowsParams p) {
     __shared__ int32_t s_ids[8][kLossMaxK];
-    __shared__ int s_count;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int r0 = blockIdx.x * ROWS_PER_BLOCK;
-    if (threadIdx.x == 0) {
-        s_count = 0;
-        if (blockIdx.x == 0) { p.ctrl->status = WIND_OK; p.ctrl->n_rows = 0; }
+    const int r = blockIdx.x * 8 + warp;
+    if (r >= p.N) return;
+    int32_t* list = s_ids[warp];
+    const int32_t* ids = p.ids + (size_t)r * p.K;
+    const float* y = p.y + (size_t)r * p.K;
+    float top = -CUDART_INF_F;
+    int flags = 0;   // 1: an entry outside the outputs, 2: NaN
+    for (int k = lane; k < p.K; k += 32) {
+        const int id = ids[k];
+        const float v = y[k];
+        if (id < -1 || id >= p.n_out) flags |= 1;
+        const bool there = id >= 0 && id < p.n_out;
+        if (there && v != v) flags |= 2;
+        if (there) top = fmaxf(top, v);
+        list[k] = there ? id : 0x7fffffff;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        flags |= __shfl_xor_sync(0xffffffffu, flags, o);
+    }
+    __syncwarp();
+    float sum = 0.f;
+    for (int k = lane; k < p.K; k += 32)
+        if (list[k] != 0x7fffffff && y[k] != -CUDART_INF_F) sum += expf((y[k] - top) / p.tau);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float log_sum = logf(sum);
+    float ent = 0.f;
+    for (int k = lane; k < p.K; k += 32) {
+        const int id = list[k];
+        float q = 0.f;
+        if (id != 0x7fffffff && y[k] != -CUDART_INF_F) {
+            const float d = (y[k] - top) / p.tau;
+            q = expf(d) / sum;
+            if (q != 0.f) ent += q * (d - log_sum);
+        }
+        int place = 0;
+#pragma unroll 4
+        for (int j = 0; j < p.K; ++j) place += list[j] < id || (list[j] == id && j < k);
+        p.sid[(size_t)r * p.K + place] = id;
+        p.sq[(size_t)r * p.K + place] = q;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ent += __shfl_xor_sync(0xffffffffu, ent, o);
+    if (lane == 0) {
+        p.mark[r] = (flags & 1) ? ROW_BAD : ((flags & 2) || top != -CUDART_INF_F ? ROW_COUNTS : ROW_NONE);
+        p.ent[r] = ent;
+    }
+}
+
+constexpr int COUNTED_BAD = 1 << 30;   // a row among them is none
+
+// Rows that count, of every ROWS_COUNTED rows: only for calls so long that the blocks of loss_gather should not count them all.
+__global__ void __launch_bounds__(256) loss_count_kernel(const RowsParams p) {
+    __shared__ int s_count;
+    if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
-    if (p.K == 0) {
-        if (threadIdx.x < ROWS_PER_BLOCK && r0 + (int)threadIdx.x < p.N) {
-            const int t = p.target[r0 + threadIdx.x];
-            const uint8_t m = t == -1 ? ROW_NONE : (t >= 0 && t < p.n_out ? ROW_COUNTS : ROW_BAD);
-            p.mark[r0 + threadIdx.x] = m;
-            if (m == ROW_COUNTS) atomicAdd(&s_count, 1);
-        }
-    } else {
-        int32_t* list = s_ids[warp];
-        for (int r = r0 + warp; r < min(r0 + ROWS_PER_BLOCK, p.N); r += 8) {
-            const int32_t* ids = p.ids + (size_t)r * p.K;
-            const float* y = p.y + (size_t)r * p.K;
-            float top = -CUDART_INF_F;
-            int flags = 0;   // 1: an entry outside the outputs, 2: NaN
-            __syncwarp();
-            for (int k = lane; k < p.K; k += 32) {
-                const int id = ids[k];
-                const float v = y[k];
-                if (id < -1 || id >= p.n_out) flags |= 1;
-                const bool there = id >= 0 && id < p.n_out;
-                if (there && v != v) flags |= 2;
-                if (there) top = fmaxf(top, v);
-                list[k] = there ? id : 0x7fffffff;
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                flags |= __shfl_xor_sync(0xffffffffu, flags, o);
-            }
-            __syncwarp();
-            float sum = 0.f;
-            for (int k = lane; k < p.K; k += 32)
-                if (list[k] != 0x7fffffff && y[k] != -CUDART_INF_F) sum += expf((y[k] - top) / p.tau);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float log_sum = logf(sum);
-            float ent = 0.f;
-            for (int k = lane; k < p.K; k += 32) {
-                const int id = list[k];
-                float q = 0.f;
-                if (id != 0x7fffffff && y[k] != -CUDART_INF_F) {
-                    const float d = (y[k] - top) / p.tau;
-                    q = expf(d) / sum;
-                    if (q != 0.f) ent += q * (d - log_sum);
-                }
-                int place = 0;
-                for (int j = 0; j < p.K; ++j) place += list[j] < id || (list[j] == id && j < k);
-                p.sid[(size_t)r * p.K + place] = id;
-                p.sq[(size_t)r * p.K + place] = q;
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) ent += __shfl_xor_sync(0xffffffffu, ent, o);
-            if (lane == 0) {
-                const uint8_t m = (flags & 1) ? ROW_BAD : ((flags & 2) || top != -CUDART_INF_F ? ROW_COUNTS : ROW_NONE);
-                p.mark[r] = m;
-                p.ent[r] = ent;
-                if (m == ROW_COUNTS) atomicAdd(&s_count, 1);
-            }
-        }
+    int n = 0, bad = 0;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < ROWS_COUNTED; i += 256) {
+        const int r = blockIdx.x * ROWS_COUNTED + i;
+        const uint8_t m = r < p.N ? row_mark(p, r) : (uint8_t)ROW_NONE;
+        n += m == ROW_COUNTS;
+        bad |= m == ROW_BAD;
     }
+    atomicAdd(&s_count, n);
+    if (bad) atomicOr(&s_count, COUNTED_BAD);
     __syncthreads();
     if (threadIdx.x == 0) p.counts[blockIdx.x] = s_count;
 }
@@ -255,40 +264,59 @@ __device__ __forceinline__ void store_one(void* row, int c, float v) {
     else static_cast<__nv_bfloat16*>(row)[c] = __float2bfloat16_rn(v);
 }
 
+// A block takes per_block rows, a warp a row at a time.  Where its first row that counts goes is the number of such rows before it,
+// which every block finds out for itself: reading up to ROWS_COUNTED marks from L2 is quicker than another launch.
 template <bool F32>
 __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
-    __shared__ int s_warp[8], s_pos[ROWS_PER_BLOCK], s_total;
-    __shared__ uint8_t s_mark[ROWS_PER_BLOCK];
+    __shared__ int s_before[8], s_pos[256];
+    __shared__ uint32_t s_ballot[8];
+    __shared__ uint8_t s_mark[256];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int r0 = blockIdx.x * ROWS_PER_BLOCK;
-    int before = 0;
-    for (int i = threadIdx.x; i < (int)blockIdx.x; i += 256) before += p.counts[i];
+    const int r0 = blockIdx.x * p.per_block, r1 = min(r0 + p.per_block, p.N);
+    int before = 0, first = 0;
+    bool bad = false;
+    if (p.counted) {
+        first = r0 / ROWS_COUNTED;
+        for (int i = threadIdx.x; i < first; i += 256) {
+            before += p.counts[i] & (COUNTED_BAD - 1);
+            bad |= (p.counts[i] & COUNTED_BAD) != 0;
+        }
+        first *= ROWS_COUNTED;
+    }
+#pragma unroll 8
+    for (int r = first + (int)threadIdx.x; r < r0; r += 256) {
+        const uint8_t m = row_mark(p, r);
+        before += m == ROW_COUNTS;
+        bad |= m == ROW_BAD;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-    if (lane == 0) s_warp[warp] = before;
-    if (threadIdx.x < ROWS_PER_BLOCK) s_mark[threadIdx.x] = r0 + (int)threadIdx.x < p.N ? p.mark[r0 + threadIdx.x] : (uint8_t)ROW_NONE;
-    __syncthreads();
-    if (warp == 0) {
-        int base = lane < 8 ? s_warp[lane] : 0;
+    const uint8_t mine = r0 + (int)threadIdx.x < r1 ? row_mark(p, r0 + threadIdx.x) : (uint8_t)ROW_NONE;
+    const uint32_t ballot = __ballot_sync(0xffffffffu, mine == ROW_COUNTS);
+    if (lane == 0) { s_before[warp] = before; s_ballot[warp] = ballot; }
+    s_mark[threadIdx.x] = mine;
+    bad = __syncthreads_or(bad || mine == ROW_BAD);
+    int base = 0, total = 0;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) base += __shfl_xor_sync(0xffffffffu, base, o);
-        const uint32_t lo = __ballot_sync(0xffffffffu, s_mark[lane] == ROW_COUNTS), hi = __ballot_sync(0xffffffffu, s_mark[lane + 32] == ROW_COUNTS);
-        const uint32_t bad = __ballot_sync(0xffffffffu, s_mark[lane] == ROW_BAD || s_mark[lane + 32] == ROW_BAD);
-        const uint32_t below = (1u << lane) - 1u;
-        s_pos[lane] = base + __popc(lo & below);
-        s_pos[lane + 32] = base + __popc(lo) + __popc(hi & below);
-        if (lane == 0) {
-            s_total = base + __popc(lo) + __popc(hi);
-            if (bad) atomicCAS(&p.ctrl->status, 0, (int)WIND_ERR_INVALID_ARG);
-        }
+    for (int i = 0; i < 8; ++i) {
+        base += s_before[i] + (i < warp ? __popc(s_ballot[i]) : 0);
+        total += s_before[i] + __popc(s_ballot[i]);
     }
+    s_pos[threadIdx.x] = base + __popc(ballot & ((1u << lane) - 1u));
     __syncthreads();
     const size_t plane = (size_t)p.Npad * p.Hp;
     const size_t es = F32 ? 4 : 2;
-    for (int i = warp; i < ROWS_PER_BLOCK && r0 + i < p.N; i += 8) {
+    for (int i = warp; r0 + i < r1; i += 8) {
         const int r = r0 + i;
         if (s_mark[i] == ROW_COUNTS) {
             const int j = s_pos[i];
+            const uint8_t* row = static_cast<const uint8_t*>(p.x) + (size_t)r * p.ldx * es;
+#pragma unroll 4
+            for (int c = lane * 8; c < p.Hp; c += 256) {
+                float v[8];
+                load8<F32>(row, c, p.H, p.x_vec, v);
+                store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, v);
+            }
             if (lane == 0) {
                 p.src[j] = r;
                 if (p.K == 0) p.target_c[j] = p.target[r];
@@ -296,12 +324,6 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
                     p.scale_c[j] = (p.dloss ? p.dloss[r] : 1.f) * p.tau;
                     p.nlse_c[j] = p.lse[r];
                 }
-            }
-            const uint8_t* row = static_cast<const uint8_t*>(p.x) + (size_t)r * p.ldx * es;
-            for (int c = lane * 8; c < p.Hp; c += 256) {
-                float v[8];
-                load8<F32>(row, c, p.H, p.x_vec, v);
-                store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, v);
             }
         } else {
             const float fill = s_mark[i] == ROW_BAD ? CUDART_NAN_F : 0.f;
@@ -315,10 +337,12 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
     }
     if (blockIdx.x == gridDim.x - 1) {
         // the last row tile is full of zeros behind the last row
-        const int n = s_total;
-        if (threadIdx.x == 0) p.ctrl->n_rows = n;
+        if (threadIdx.x == 0) {   // (this block has seen every mark)
+            p.ctrl->status = bad ? WIND_ERR_INVALID_ARG : WIND_OK;
+            p.ctrl->n_rows = total;
+        }
         const float zero[8] = {};
-        for (int j = n + warp; j < (n + 127) / 128 * 128; j += 8)
+        for (int j = total + warp; j < (total + 127) / 128 * 128; j += 8)
             for (int c = lane * 8; c < p.Hp; c += 256) store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, zero);
     }
 }
@@ -811,13 +835,14 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 // ---------------------------------------------------------------------------
 // what is left
 // ---------------------------------------------------------------------------
-// 32 rows x 8 slices of the partial results a block.
+// 8 rows x 32 slices of the partial results a block: eight neighbouring rows are a sector of 32 bytes, and a slice is short (a text
+// model's 512 parts: 16 steps; with 32 rows x 8 slices it took 51 us instead of 9).
 __global__ void __launch_bounds__(256) loss_combine_kernel(const LossCtrl* ctrl, const int32_t* src, const float* pm, const float* ps, const float* pq,
                                                            int parts, int Npad, const float* ent, float tau, float* loss, float* lse) {
-    __shared__ float s_m[8][32], s_s[8][32], s_q[8][32];
-    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-    const int j = blockIdx.x * 32 + lane, n = ctrl->n_rows;
-    if ((int)blockIdx.x * 32 >= n) return;
+    __shared__ float s_m[32][8], s_s[32][8], s_q[32][8];
+    const int at_row = threadIdx.x & 7, slice = threadIdx.x >> 3;
+    const int j = blockIdx.x * 8 + at_row, n = ctrl->n_rows;
+    if ((int)blockIdx.x * 8 >= n) return;
     float m = -CUDART_INF_F, s = 0.f, qz = 0.f;
     auto add = [&](float m2, float s2) {
         const float m1 = fmaxf(m, m2), base = m1 == -CUDART_INF_F ? 0.f : m1;
@@ -825,18 +850,29 @@ __global__ void __launch_bounds__(256) loss_combine_kernel(const LossCtrl* ctrl,
         m = m1;
     };
     if (j < n)
-        for (int i = slice; i < parts; i += 8) {
+#pragma unroll 4
+        for (int i = slice; i < parts; i += 32) {
             const size_t at = (size_t)i * Npad + j;
             add(pm[at], ps[at]);
             qz += pq[at];
         }
-    s_m[slice][lane] = m; s_s[slice][lane] = s; s_q[slice][lane] = qz;
+    s_m[slice][at_row] = m; s_s[slice][at_row] = s; s_q[slice][at_row] = qz;
     __syncthreads();
-    if (slice || j >= n) return;
-    for (int i = 1; i < 8; ++i) {
-        add(s_m[i][lane], s_s[i][lane]);
-        qz += s_q[i][lane];
+    if (threadIdx.x >= 32) return;
+    // lane = 8 * quarter + row: eight slices each, then the quarters
+    m = -CUDART_INF_F; s = 0.f; qz = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int k = (threadIdx.x >> 3) * 8 + i;
+        add(s_m[k][at_row], s_s[k][at_row]);
+        qz += s_q[k][at_row];
     }
+#pragma unroll
+    for (int o = 8; o < 32; o <<= 1) {
+        add(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
+        qz += __shfl_xor_sync(0xffffffffu, qz, o);
+    }
+    if (threadIdx.x >= 8 || j >= n) return;
     const int r = src[j];
     const float log_s = logf(s);
     // (maximum minus the targets' mean logit first: both are large where the logits are)
@@ -995,9 +1031,17 @@ cudaError_t loss_run(const LossCall& c) {
     r.ent = reinterpret_cast<float*>(c.ws + L.ent);
     r.xc = reinterpret_cast<__nv_bfloat16*>(c.ws + L.x);
     r.loss = c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.dloss; r.dx = c.dx; r.lddx = c.lddx;
-    const int row_blocks = cdiv(c.N, ROWS_PER_BLOCK);
-    loss_mark_kernel<<<row_blocks, 256, 0, c.stream>>>(r);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (c.K) {
+        loss_list_kernel<<<cdiv(c.N, 8), 256, 0, c.stream>>>(r);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    }
+    r.counted = c.N > ROWS_COUNTED;
+    if (r.counted) {
+        loss_count_kernel<<<cdiv(c.N, ROWS_COUNTED), 256, 0, c.stream>>>(r);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    }
+    r.per_block = std::min(256, up(cdiv(c.N, 16 * sms), 8));   // a block's warps take one row each while that fills the chip
+    const int row_blocks = cdiv(c.N, r.per_block);
     if (f32) loss_gather_kernel<true><<<row_blocks, 256, 0, c.stream>>>(r);
     else loss_gather_kernel<false><<<row_blocks, 256, 0, c.stream>>>(r);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
@@ -1034,7 +1078,7 @@ cudaError_t loss_run(const LossCall& c) {
         const int grid = (int)std::min<long long>((long long)row_tiles * p.n_vt, sms);
         loss_kernel_of(FORWARD, c.K > 0, L.planes)<<<grid, LT_THREADS, kLossSmem, c.stream>>>(map_x, map_w, map_x, map_w, p);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        loss_combine_kernel<<<cdiv(c.N, 32), 256, 0, c.stream>>>(ctrl, r.src, p.pm, p.ps, p.pq, cdiv(c.o.n_out, 128), L.Npad,
+        loss_combine_kernel<<<cdiv(c.N, 8), 256, 0, c.stream>>>(ctrl, r.src, p.pm, p.ps, p.pq, cdiv(c.o.n_out, 128), L.Npad,
                                                                   c.K ? r.ent : nullptr, c.tau, c.loss, c.lse_out);
         return cudaGetLastError();
     }
