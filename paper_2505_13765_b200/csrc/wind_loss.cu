@@ -43,10 +43,6 @@ namespace wind {
 // ---------------------------------------------------------------------------
 // sizes
 // ---------------------------------------------------------------------------
-constexpr int LT_N = 256;                 // columns of an output tile (BM = 128 rows)
-constexpr int LT_STAGES = 4;
-constexpr uint32_t LT_STAGE_BYTES = A_STAGE_BYTES + LT_N * BK * 2;
-constexpr int LT_THREADS = 64 + 256;      // warp 0: TMA, warp 1: MMA + tensor memory, warps 2..9: epilogue
 constexpr int LT_BAND = 16;               // row tiles that are worked on together (see tile_of)
 constexpr int ROWS_COUNTED = 8192;        // longer calls have the rows that count counted by a kernel of its own, so many at a time
 constexpr int PANEL_BYTES = 64 * BK * 2;  // 64 x 64 bf16
@@ -54,60 +50,6 @@ constexpr int kFillCtas = 148;            // CTAs that a product is cut for
 
 static inline int up(long long a, int b) { return (int)((a + b - 1) / b * b); }
 static inline int cdiv(long long a, int b) { return (int)((a + b - 1) / b); }
-
-LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad) {
-    LossLayout L{};
-    const bool f32 = o.dtype == WIND_DT_F32;
-    L.planes = f32 ? 3 : 1;
-    L.pack_w = f32 || o.H % 8 || o.ldw % 8 || (o.n_out > 1 && o.ldw < o.H) || reinterpret_cast<uintptr_t>(o.w) % 16;
-    L.Hp = up(o.H, 64);
-    L.Npad = up(N, 128);
-    size_t off = 0;
-    auto take = [&](size_t bytes) { size_t at = off; off = align_up(off + bytes); return at; };
-    L.ctrl = take(sizeof(LossCtrl));
-    const size_t np = (size_t)L.Npad;
-    L.counts = take(N > ROWS_COUNTED ? 4 * (size_t)cdiv(N, ROWS_COUNTED) : 0);
-    L.mark = take(K ? np : 0);
-    L.src = take(4 * np);
-    L.target = take(K ? 0 : 4 * np);
-    L.scale = take(grad ? 4 * np : 0);
-    L.nlse = take(grad ? 4 * np : 0);
-    L.sid = take(4 * (size_t)N * K);
-    L.sq = take(4 * (size_t)N * K);
-    L.ent = take(K ? 4 * np : 0);
-    L.x = take(2 * (size_t)L.planes * np * L.Hp);
-    L.w = take(L.pack_w ? 2 * (size_t)L.planes * o.n_out * L.Hp : 0);
-    if (!grad) {
-        const size_t parts = (size_t)cdiv(o.n_out, 128);
-        L.pm = take(4 * parts * np);
-        L.ps = take(4 * parts * np);
-        L.pq = take(4 * parts * np);
-    } else {
-        // a piece: as many outputs as keep its g within kLossPieceBytes, 2048 at least (below that the partial sums of dx, read and
-        // written once a piece, cost more than a few per cent of the products)
-        const long long all = up(o.n_out, LT_N);
-        const long long fit = (long long)(kLossPieceBytes / (2 * (size_t)L.planes * (np ? np : 1))) / LT_N * LT_N;
-        L.piece = (int)std::min(all, std::max(2048LL, fit));
-        L.pieces = cdiv(o.n_out, L.piece);
-        const int ht = cdiv(o.H, LT_N), terms = f32 ? 6 : 1;
-        const long long t_dx = (long long)(L.Npad / 128) * ht, t_dw = (long long)cdiv(std::min(o.n_out, L.piece), 128) * ht;
-        const int kb_dx = cdiv(std::min(o.n_out, L.piece), BK), kb_dw = L.Npad / BK;
-        auto parts_of = [&](long long tiles, int kb) {
-            if (tiles <= 0 || tiles >= kFillCtas) return 1;
-            return (int)std::max(1LL, std::min<long long>({kFillCtas / tiles, (long long)kb * terms / 8, (long long)kb}));
-        };
-        L.s_dx = parts_of(t_dx, kb_dx);
-        L.s_dw = parts_of(t_dw, kb_dw);
-        L.slab_dx = L.s_dx > 1 || L.pieces > 1;
-        L.slab_dw = L.s_dw > 1;
-        L.g = take(2 * (size_t)L.planes * np * L.piece);
-        L.dbp = take(4 * (np / 128) * L.piece);
-        L.sdx = take(L.slab_dx ? 4 * (size_t)L.s_dx * np * L.Hp : 0);
-        L.sdw = take(L.slab_dw ? 4 * (size_t)L.s_dw * L.piece * L.Hp : 0);
-    }
-    L.total = off;
-    return L;
-}
 
 // ---------------------------------------------------------------------------
 // rows: which count, and their operands
@@ -258,6 +200,32 @@ __device__ __forceinline__ void store8(__nv_bfloat16* dst, size_t plane, const f
     }
 }
 
+// 256-bit store: a whole sector per thread (16-byte stores from 32 threads to 32 rows send every byte to L2 twice)
+__device__ __forceinline__ void store_sector(void* p, const uint32_t* w) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+
+// Sixteen neighbouring values in one to three bf16 parts, 32-byte aligned.
+template <int PARTS>
+__device__ __forceinline__ void store16(__nv_bfloat16* dst, size_t plane, const float* v) {
+    uint32_t w[PARTS][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (PARTS == 1) w[0][i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        else {
+            float a[3], b[3];
+            split3(v[2 * i], a);
+            split3(v[2 * i + 1], b);
+#pragma unroll
+            for (int t = 0; t < PARTS; ++t) w[t][i] = pack_bf16x2(a[t], b[t]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < PARTS; ++t) store_sector(dst + t * plane, w[t]);
+}
+
 template <bool F32>
 __device__ __forceinline__ void store_one(void* row, int c, float v) {
     if (F32) static_cast<float*>(row)[c] = v;
@@ -364,12 +332,15 @@ __global__ void __launch_bounds__(256) loss_pack_kernel(const void* w, int64_t l
 // The products: a persistent tcgen05 GEMM with three epilogues
 // ---------------------------------------------------------------------------
 enum LossMode { FORWARD = 0, LOGITS = 1, PRODUCTS = 2 };
+// Operands: bf16; bf16 with g in two parts, for calls of few rows; fp32 (three parts of every operand).
+enum LossKind { BF16 = 1, BF16_FINE = 2, F32 = 3 };
 
 struct LossGemm {
     LossCtrl* ctrl;
     int n_out, H, Hp, Npad, K;
     int kb;                       // K blocks of the logits
-    int v0, cols, n_vt;           // this piece's first output, its outputs (to n_out at most) and 256-column tiles
+    int tn;                       // columns of a tile: 64, 128 or 256
+    int v0, cols, n_vt;           // this piece's first output, its outputs (to n_out at most) and tiles
     float rtau;                   // 1 / tau
     const float* bias;
     const int32_t* src; const int32_t* target; const int32_t* sid; const float* sq;
@@ -377,15 +348,32 @@ struct LossGemm {
     const float* scale; const float* nlse;
     __nv_bfloat16* g; int ldg; size_t g_plane; float* dbp;   // LOGITS
     // PRODUCTS
-    int ht, s_dx, s_dw, add_dx;   // 256-column tiles of H, parts of the sums, whether dx's partial sums are added to
+    int ht, s_dx, s_dw, add_dx;   // tiles of H, parts of the sums, whether dx's partial sums are added to
     float *sdx, *sdw; int slab_rows_dw;   // partial sums, or null: straight to dx / dw
-    void* dx; int64_t lddx; int dx_vec; int want_dx;
+    void* dx; int64_t lddx; int dx_vec; int want_dx;         // vec: what rows are aligned to, 0: nothing, 1: 16 bytes, 2: 32 bytes
     void* dw; int64_t lddw; int dw_vec; int want_dw;
 };
 
-// Operand parts of the six products of fp32 models, smallest first (bf16 models: the last one alone).
-__device__ __forceinline__ int term_a(int t) { return (0x001102 >> (4 * t)) & 3; }   // 2 0 1 1 0 0
-__device__ __forceinline__ int term_b(int t) { return (0x010120 >> (4 * t)) & 3; }   // 0 2 1 0 1 0
+// Shape of a kernel.  A stage holds a K block of every part of both operands, and all part products are made from it: fp32 fetches 96 KB
+// for six products of 128 x 128 x 64 (64 bytes of L2 a cycle and SM; a fetch for each product would be 128).
+template <int MODE, int KIND>
+struct Shape {
+    static constexpr int TN = KIND == F32 ? 128 : 256;                                       // most columns of a tile (BM = 128 rows)
+    static constexpr int A_PARTS = KIND == F32 ? 3 : (KIND == BF16_FINE && MODE == PRODUCTS ? 2 : 1), B_PARTS = KIND == F32 ? 3 : 1;
+    static constexpr int TERMS = KIND == F32 ? 6 : A_PARTS;
+    static constexpr int B_BYTES = TN * BK * 2;
+    static constexpr int STAGE_BYTES = A_PARTS * A_STAGE_BYTES + B_PARTS * B_BYTES;
+    static constexpr int STAGES = 196608 / STAGE_BYTES;                                      // 4, 3 (fine) or 2 (fp32)
+    // Groups of four epilogue warps (one per tensor-memory lane quadrant), each with its columns of a tile.  The gradient's share of
+    // logits takes more of the ALUs than the softmax's sums do: 16 warps hide more of it than 8.
+    static constexpr int GROUPS = MODE == LOGITS && KIND != F32 ? 4 : 2;
+    static constexpr int EPI = 128 * GROUPS, THREADS = 64 + EPI, CHUNKS = TN / GROUPS / 32;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
+    // Part products, smallest first: the parts of A and B of each (fp32: 20 02 11 10 01 00; fine: 10 00).
+    static __device__ __forceinline__ constexpr int a_part(int t) { return KIND == F32 ? (0x001102 >> (4 * t)) & 3 : TERMS - 1 - t; }
+    static __device__ __forceinline__ constexpr int b_part(int t) { return KIND == F32 ? (0x010120 >> (4 * t)) & 3 : 0; }
+};
+__host__ __device__ constexpr int group_cols(int tn, int groups) { return tn / groups > 32 ? tn / groups : 32; }
 
 // K-major tiles as in smem_desc_sw128.  MN-major ones: panels of 64 (M or N) x 64 (K) bf16, a K row of a panel being 128 bytes: 8 K rows
 // are a swizzle atom of 1024 bytes (stride byte offset), panels stand PANEL_BYTES apart (leading byte offset).
@@ -399,8 +387,11 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t smem_addr) {
     return d;
 }
 
+// The instruction wants the whole warp at once, and a vote does not bring lanes together that took different ways before, as they do
+// out of a long wait on an mbarrier: they meet here.
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
     uint32_t r[32];
+    __syncwarp();
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
         "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -469,7 +460,7 @@ __device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long
     const int r = (int)(u - (long long)t.part * tiles);
     t.mt = r / p.ht;
     t.nt = r - t.mt * p.ht;
-    const int kb = t.dw ? (n_rows + BK - 1) / BK : p.n_vt * (LT_N / BK), s = t.dw ? p.s_dw : p.s_dx;
+    const int kb = ((t.dw ? n_rows : p.cols) + BK - 1) / BK, s = t.dw ? p.s_dw : p.s_dx;
     t.k0 = (int)((long long)kb * t.part / s);
     t.nk = (int)((long long)kb * (t.part + 1) / s) - t.k0;
     return t;
@@ -477,53 +468,77 @@ __device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long
 
 template <int MODE>
 __device__ __forceinline__ int unit_cols(const LossGemm& p, const Unit& t) {   // columns of B that are there
-    return min(LT_N, (MODE == PRODUCTS ? p.H : p.cols) - t.nt * LT_N);
+    return MODE == PRODUCTS ? min(p.tn, p.H - t.nt * p.tn) : min(p.tn, p.cols - t.nt * p.tn);
 }
 
-// FORWARD epilogue of one row's 128 columns from `col` (an output) on.
+// 32 columns of an accumulator row: from tensor memory, or (fp32) from the sums in registers.
+template <int KIND>
+__device__ __forceinline__ void fetch32(float* v, uint32_t taddr, const float* sums, int c) {
+    if constexpr (KIND == F32) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = sums[c * 32 + i];
+    } else {
+        tmem_ld32(taddr + c * 32, v);
+    }
+}
+
+// A row's target distribution, met along its columns.
 template <bool LIST>
-__device__ __forceinline__ void forward_row(const LossGemm& p, uint32_t taddr, const float* bias, int col, int n_cols, int row, int n_rows, int part) {
-    float m = -CUDART_INF_F, s = 0.f, qz = 0.f;
-    int target = -1, cur = 0, next = 0x7fffffff;
+struct Targets {
+    int next = 0x7fffffff, cur = 0, K;
     const int32_t* sid = nullptr;
     const float* sq = nullptr;
-    if (row < n_rows) {
-        if (!LIST) target = p.target[row];
-        else {
-            const size_t at = (size_t)p.src[row] * p.K;
-            sid = p.sid + at;
-            sq = p.sq + at;
-            int lo = 0, hi = p.K;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (sid[mid] < col) lo = mid + 1; else hi = mid;
+    __device__ __forceinline__ Targets(const LossGemm& p, int row, bool there, int col) : K(p.K) {
+        if (!there) return;
+        if (!LIST) { next = p.target[row]; return; }
+        const size_t at = (size_t)p.src[row] * K;
+        sid = p.sid + at;
+        sq = p.sq + at;
+        int lo = 0, hi = K;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (sid[mid] < col) lo = mid + 1; else hi = mid;
+        }
+        cur = lo;
+        if (cur < K) next = sid[cur];
+    }
+    // f(column, weight) for the targets in [col, col + 32)
+    template <typename F>
+    __device__ __forceinline__ void in(int col, F f) {
+        if (!LIST) {
+            if (next >= col && next < col + 32) f(next - col, 1.f);
+        } else {
+            while (next < col + 32) {
+                f(next - col, sq[cur]);
+                ++cur;
+                next = cur < K ? sid[cur] : 0x7fffffff;
             }
-            cur = lo;
-            if (cur < p.K) next = sid[cur];
         }
     }
-#pragma unroll 1
-    for (int c0 = 0; c0 < n_cols; c0 += 32) {
+};
+
+// FORWARD epilogue of one row's columns (n_cols of them are outputs) from `col` on.
+template <bool LIST, int KIND, int CHUNKS>
+__device__ __forceinline__ void forward_row(const LossGemm& p, uint32_t taddr, const float* sums, const float* bias, int col, int n_cols, int row,
+                                            int n_rows, int part) {
+    float m = -CUDART_INF_F, s = 0.f, qz = 0.f;
+    Targets<LIST> targets(p, row, row < n_rows, col);
+    constexpr int UNROLL = KIND == F32 ? CHUNKS : 1;
+#pragma unroll UNROLL
+    for (int c = 0; c < CHUNKS; ++c) {
+        if (c * 32 >= n_cols) continue;
         float v[32];
-        __syncwarp();
-        tmem_ld32(taddr + c0, v);
+        fetch32<KIND>(v, taddr, sums, c);
         float top = -CUDART_INF_F;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            v[i] = (v[i] + bias[c0 + i]) * p.rtau;
+            v[i] = (v[i] + bias[c * 32 + i]) * p.rtau;
             top = fmaxf(top, v[i]);
         }
-        if (!LIST) {
-            const int at = target - (col + c0);
-            if (at >= 0 && at < 32) qz = pick32(v, at);
-        } else {
-            while (next < col + c0 + 32) {
-                const float q = sq[cur], z = pick32(v, next - (col + c0));
-                if (q != 0.f) qz += q * z;
-                ++cur;
-                next = cur < p.K ? sid[cur] : 0x7fffffff;
-            }
-        }
+        targets.in(col + c * 32, [&](int at, float q) {
+            const float z = pick32(v, at);
+            if (q != 0.f) qz += q * z;
+        });
         const float m1 = fmaxf(m, top), base = m1 == -CUDART_INF_F ? 0.f : m1;
         float add = 0.f;
 #pragma unroll
@@ -553,108 +568,95 @@ __device__ __forceinline__ float column_sums(float* v, int lane) {
     return v[0];
 }
 
-// LOGITS epilogue of one row's 128 columns: g, and the warp's share of the columns' sums.
-template <bool LIST, int P>
-__device__ __forceinline__ void logits_row(const LossGemm& p, uint32_t taddr, const float* bias, int col, int g_col, int row, int n_rows, float* sums) {
-    const int lane = threadIdx.x & 31;
+// LOGITS epilogue of one row's columns: g, to the next multiple of 64 outputs (K blocks of the product behind), and the warp's share of
+// the columns' sums.
+template <bool LIST, int KIND, int CHUNKS>
+__device__ __forceinline__ void logits_row(const LossGemm& p, uint32_t taddr, const float* sums, const float* bias, int g_col, int n_cols, int row,
+                                           int n_rows, float* col_sums) {
+    const int lane = threadIdx.x & 31, col = p.v0 + g_col;
     const bool there = row < n_rows;
     const float scale = there ? p.scale[row] : 0.f, nlse = there ? p.nlse[row] : 0.f;
-    int target = -1, cur = 0, next = 0x7fffffff;
-    const int32_t* sid = nullptr;
-    const float* sq = nullptr;
-    if (there) {
-        if (!LIST) target = p.target[row];
-        else {
-            const size_t at = (size_t)p.src[row] * p.K;
-            sid = p.sid + at;
-            sq = p.sq + at;
-            int lo = 0, hi = p.K;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (sid[mid] < col) lo = mid + 1; else hi = mid;
-            }
-            cur = lo;
-            if (cur < p.K) next = sid[cur];
-        }
-    }
+    Targets<LIST> targets(p, row, there, col);
     __nv_bfloat16* dst = p.g + (size_t)row * p.ldg + g_col;
-#pragma unroll 1
-    for (int c0 = 0; c0 < 128; c0 += 32) {
+    const int g_end = (p.cols + 63) / 64 * 64 - g_col;
+    constexpr int UNROLL = KIND == F32 ? CHUNKS : 1;
+#pragma unroll UNROLL
+    for (int c = 0; c < CHUNKS; ++c) {
+        if (c * 32 >= n_cols || c * 32 >= g_end) continue;
         float v[32];
-        __syncwarp();
-        const bool any = there && col + c0 < p.n_out;   // (behind the outputs the accumulator holds what an earlier tile left)
-        tmem_ld32(taddr + c0, v);
+        const bool some = col + c * 32 < p.n_out;   // (behind the outputs the accumulator holds what an earlier tile left)
+        if (some) {
+            fetch32<KIND>(v, taddr, sums, c);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = scale * exp2_fast(((v[i] + bias[c0 + i]) * p.rtau - nlse) * kLog2e);
-        if (!LIST) {
-            const int at = target - (col + c0);
-            if (at >= 0 && at < 32) {
+            for (int i = 0; i < 32; ++i) v[i] = scale * exp2_fast(((v[i] + bias[c * 32 + i]) * p.rtau - nlse) * kLog2e);
+            targets.in(col + c * 32, [&](int at, float q) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = at == i ? v[i] - scale : v[i];
-            }
-        } else {
-            while (next < col + c0 + 32) {
-                const float q = scale * sq[cur];
-                const int at = next - (col + c0);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = at == i ? v[i] - q : v[i];
-                ++cur;
-                next = cur < p.K ? sid[cur] : 0x7fffffff;
-            }
+                for (int i = 0; i < 32; ++i) v[i] = at == i ? v[i] - scale * q : v[i];
+            });
         }
-        if (!any) {
+        if (!there || !some) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
         }
-        if (P == 1) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) store8<false>(dst + c0 + i, 0, v + i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) store8<true>(dst + c0 + i, p.g_plane, v + i);
-        }
+        for (int i = 0; i < 32; i += 16) store16<KIND>(dst + c * 32 + i, p.g_plane, v + i);
         if (p.dbp) {
+            __syncwarp();
             const float sum = column_sums(v, lane);
-            sums[c0 + lane] = sum;
+            col_sums[c * 32 + lane] = sum;
         }
     }
 }
 
-// PRODUCTS epilogue of one row's columns [h, H) that belong to its half of the tile; zero: the sum has no term.
-template <bool F32>
-__device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, uint32_t taddr, int half, int row_in_tile, int n_rows, bool zero) {
+// PRODUCTS epilogue of one row's columns from h0 on; zero: the sum has no term.
+template <int KIND, int CHUNKS>
+__device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, uint32_t taddr, const float* sums, int h0, int row_in_tile, int n_rows,
+                                            bool zero) {
+    constexpr bool f32 = KIND == F32;
     const int row = t.mt * BM + row_in_tile;                       // of dx: a gathered row; of dW: an output of the piece
     const bool there = row < (t.dw ? p.cols : n_rows);
     float* slab = t.dw ? p.sdw : p.sdx;
-    const int h0 = t.nt * LT_N + half * 128, h1 = min(h0 + 128, slab ? p.Hp : p.H);
+    const int h1 = slab ? p.Hp : p.H;
     uint8_t* out = nullptr;
     float* sum = nullptr;
     if (there) {
         if (slab) sum = slab + ((size_t)t.part * (t.dw ? p.slab_rows_dw : p.Npad) + row) * p.Hp;
-        else if (t.dw) out = static_cast<uint8_t*>(p.dw) + (size_t)(p.v0 + row) * p.lddw * (F32 ? 4 : 2);
-        else out = static_cast<uint8_t*>(p.dx) + (size_t)p.src[row] * p.lddx * (F32 ? 4 : 2);
+        else if (t.dw) out = static_cast<uint8_t*>(p.dw) + (size_t)(p.v0 + row) * p.lddw * (f32 ? 4 : 2);
+        else out = static_cast<uint8_t*>(p.dx) + (size_t)p.src[row] * p.lddx * (f32 ? 4 : 2);
     }
-    const bool vec = t.dw ? p.dw_vec : p.dx_vec;
-#pragma unroll 1
-    for (int h = h0; h < h1; h += 32) {
+    const int vec = t.dw ? p.dw_vec : p.dx_vec;
+    constexpr int UNROLL = f32 ? CHUNKS : 1;
+#pragma unroll UNROLL
+    for (int c = 0; c < CHUNKS; ++c) {
+        const int h = h0 + c * 32;
+        if (h >= h1) continue;
         float v[32];
-        __syncwarp();
         if (zero) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
-        } else tmem_ld32(taddr + (h - h0), v);
+        } else fetch32<KIND>(v, taddr, sums, c);
         if (!there) {
         } else if (sum) {
-            float4* d = reinterpret_cast<float4*>(sum + h);
-            const bool add = !t.dw && p.add_dx;
+            if (!t.dw && p.add_dx) {
+                const float4* d = reinterpret_cast<const float4*>(sum + h);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float4 o = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                if (add) { const float4 b = d[i]; o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w; }
-                d[i] = o;
+                for (int i = 0; i < 8; ++i) {
+                    const float4 b = d[i];
+                    v[4 * i] += b.x; v[4 * i + 1] += b.y; v[4 * i + 2] += b.z; v[4 * i + 3] += b.w;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) store_sector(sum + h + i, reinterpret_cast<const uint32_t*>(v + i));
+        } else if (vec == 2 && h + 32 <= h1) {
+            if constexpr (f32) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) store_sector(reinterpret_cast<float*>(out) + h + i, reinterpret_cast<const uint32_t*>(v + i));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; i += 16) store16<1>(reinterpret_cast<__nv_bfloat16*>(out) + h + i, 0, v + i);
             }
         } else if (vec && h + 32 <= h1) {
-            if (F32) {
+            if constexpr (f32) {
                 float4* d = reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + h);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
@@ -665,31 +667,31 @@ __device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, ui
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-                if (h + i < h1) store_one<F32>(out, h + i, v[i]);
+                if (h + i < h1) store_one<f32>(out, h + i, v[i]);
         }
     }
 }
 
-template <int MODE, bool LIST, int P>
-__global__ void __launch_bounds__(LT_THREADS, 1)
+template <int MODE, bool LIST, int KIND>
+__global__ void __launch_bounds__((Shape<MODE, KIND>::THREADS), 1)
 loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a2,
                  const __grid_constant__ CUtensorMap map_b2, const LossGemm p) {
+    using S = Shape<MODE, KIND>;
+    constexpr int TN = S::TN, EPI = S::EPI, STAGES = S::STAGES, A_PARTS = S::A_PARTS, B_PARTS = S::B_PARTS;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full_bar[LT_STAGES], empty_bar[LT_STAGES], acc_full[2], acc_empty[2], drain_bar;
+    __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], acc_full[2], acc_empty[2], drain_bar;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
-    __shared__ float s_bias[2][LT_N];
-    __shared__ float s_db[8][128];
+    __shared__ float s_bias[2][TN];
+    __shared__ float s_db[4][TN];     // [lane quadrant][column of the tile]
 
     const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
     uint8_t* smem = align_smem_1024(smem_raw);
-    constexpr int TERMS = P == 3 ? 6 : 1;
-    constexpr int FIRST_TERM = 6 - TERMS;
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int s = 0; s < LT_STAGES; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], 8); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], EPI / 32); }
         mbar_init(&drain_bar, 1);
         fence_barrier_init();
         prefetch_tmap(&map_a); prefetch_tmap(&map_b);
@@ -710,36 +712,34 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 const Unit t = unit_of<MODE>(p, n_rows, u);
                 const int panels = (unit_cols<MODE>(p, t) + 63) / 64;
-                for (int term = FIRST_TERM; term < 6 && ok; ++term) {
-                    const int pa = term_a(term), pb = term_b(term);
-                    for (int kb = t.k0; kb < t.k0 + t.nk; ++kb, ++it) {
-                        const int s = it % LT_STAGES;
-                        if (!mbar_wait(&empty_bar[s], ((it / LT_STAGES) & 1) ^ 1, &abort_flag)) { ok = false; break; }
-                        uint8_t* a = smem + (size_t)s * LT_STAGE_BYTES;
-                        uint8_t* b = a + A_STAGE_BYTES;
-                        if (MODE != PRODUCTS) {
-                            mbar_expect_tx(&full_bar[s], LT_STAGE_BYTES);
-                            tma_load_3d(a, &map_a, kb * BK, t.mt * BM, pa, &full_bar[s]);
-                            tma_load_3d(b, &map_b, kb * BK, p.v0 + t.nt * LT_N, pb, &full_bar[s]);
-                        } else {
-                            mbar_expect_tx(&full_bar[s], (uint32_t)(A_STAGE_BYTES + panels * PANEL_BYTES));
-                            if (!t.dw) {
-                                tma_load_3d(a, &map_a, kb * BK, t.mt * BM, pa, &full_bar[s]);
-                                for (int q = 0; q < panels; ++q)
-                                    tma_load_3d(b + q * PANEL_BYTES, &map_b, t.nt * LT_N + q * 64, p.v0 + kb * BK, pb, &full_bar[s]);
-                            } else {
-                                for (int q = 0; q < 2; ++q)
-                                    tma_load_3d(a + q * PANEL_BYTES, &map_a2, t.mt * BM + q * 64, kb * BK, pa, &full_bar[s]);
-                                for (int q = 0; q < panels; ++q)
-                                    tma_load_3d(b + q * PANEL_BYTES, &map_b2, t.nt * LT_N + q * 64, kb * BK, pb, &full_bar[s]);
-                            }
-                        }
+                const uint32_t b_bytes = MODE == PRODUCTS ? panels * PANEL_BYTES : p.tn * BK * 2;
+                for (int kb = t.k0; kb < t.k0 + t.nk; ++kb, ++it) {
+                    const int s = it % STAGES;
+                    if (!mbar_wait(&empty_bar[s], ((it / STAGES) & 1) ^ 1, &abort_flag)) { ok = false; break; }
+                    uint8_t* a = smem + (size_t)s * S::STAGE_BYTES;
+                    uint8_t* b = a + A_PARTS * A_STAGE_BYTES;
+                    mbar_expect_tx(&full_bar[s], A_PARTS * A_STAGE_BYTES + B_PARTS * b_bytes);
+                    if (MODE != PRODUCTS) {
+                        for (int i = 0; i < A_PARTS; ++i) tma_load_3d(a + i * A_STAGE_BYTES, &map_a, kb * BK, t.mt * BM, i, &full_bar[s]);
+                        for (int i = 0; i < B_PARTS; ++i) tma_load_3d(b + i * S::B_BYTES, &map_b, kb * BK, p.v0 + t.nt * p.tn, i, &full_bar[s]);
+                    } else if (!t.dw) {
+                        for (int i = 0; i < A_PARTS; ++i) tma_load_3d(a + i * A_STAGE_BYTES, &map_a, kb * BK, t.mt * BM, i, &full_bar[s]);
+                        for (int i = 0; i < B_PARTS; ++i)
+                            for (int q = 0; q < panels; ++q)
+                                tma_load_3d(b + i * S::B_BYTES + q * PANEL_BYTES, &map_b, t.nt * p.tn + q * 64, p.v0 + kb * BK, i, &full_bar[s]);
+                    } else {
+                        for (int i = 0; i < A_PARTS; ++i)
+                            for (int q = 0; q < 2; ++q)
+                                tma_load_3d(a + i * A_STAGE_BYTES + q * PANEL_BYTES, &map_a2, t.mt * BM + q * 64, kb * BK, i, &full_bar[s]);
+                        for (int i = 0; i < B_PARTS; ++i)
+                            for (int q = 0; q < panels; ++q)
+                                tma_load_3d(b + i * S::B_BYTES + q * PANEL_BYTES, &map_b2, t.nt * p.tn + q * 64, kb * BK, i, &full_bar[s]);
                     }
                 }
             }
             if (!ok) {   // given up: the copies in flight still write into this CTA's shared memory
                 int late = 0;
-                for (uint32_t i = it > LT_STAGES ? it - LT_STAGES : 0; i < it; ++i) mbar_wait(&full_bar[i % LT_STAGES], (i / LT_STAGES) & 1, &late);
+                for (uint32_t i = it > STAGES ? it - STAGES : 0; i < it; ++i) mbar_wait(&full_bar[i % STAGES], (i / STAGES) & 1, &late);
             }
         }
     } else if (warp == 1) {
@@ -748,29 +748,33 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             bool ok = true;
             for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 const Unit t = unit_of<MODE>(p, n_rows, u);
-                if (t.nk == 0) continue;
                 const int n = (unit_cols<MODE>(p, t) + 31) / 32 * 32;   // (the epilogues read 32 columns at a time)
                 const bool a_mn = MODE == PRODUCTS && t.dw, b_mn = MODE == PRODUCTS;
                 const uint32_t idesc = idesc_bf16(BM, n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                 const uint64_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;   // 16 of K, in units of 16 bytes
-                const uint32_t acc = n_acc & 1u;
-                if (!mbar_wait(&acc_empty[acc], ((n_acc >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t tm_d = tmem_base + acc * LT_N;
-                const int blocks = t.nk * TERMS;
-                for (int i = 0; i < blocks; ++i, ++it) {
-                    const int s = it % LT_STAGES;
-                    if (!mbar_wait(&full_bar[s], (it / LT_STAGES) & 1, &abort_flag)) { ok = false; break; }
+                uint32_t tm_d = 0;
+                for (int i = 0; i < t.nk; ++i, ++it) {
+                    const uint32_t acc = n_acc & 1u;
+                    const bool first = KIND == F32 || i == 0, last = KIND == F32 || i == t.nk - 1;   // of an accumulator
+                    if (first) {
+                        if (!mbar_wait(&acc_empty[acc], ((n_acc >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                        tm_d = tmem_base + acc * TN;
+                    }
+                    const int s = it % STAGES;
+                    if (!mbar_wait(&full_bar[s], (it / STAGES) & 1, &abort_flag)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t a_addr = smem_u32(smem + (size_t)s * LT_STAGE_BYTES), b_addr = a_addr + A_STAGE_BYTES;
+                    const uint32_t a_addr = smem_u32(smem + (size_t)s * S::STAGE_BYTES), b_addr = a_addr + A_PARTS * A_STAGE_BYTES;
                     const uint64_t adesc = a_mn ? smem_desc_mn(a_addr) : smem_desc_sw128(a_addr);
                     const uint64_t bdesc = b_mn ? smem_desc_mn(b_addr) : smem_desc_sw128(b_addr);
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) tc_mma_bf16(tm_d, adesc + k * a_step, bdesc + k * b_step, idesc, (i | k) != 0);
+                    for (int term = 0; term < S::TERMS; ++term) {
+                        const uint64_t ad = adesc + S::a_part(term) * (A_STAGE_BYTES >> 4), bd = bdesc + S::b_part(term) * (S::B_BYTES >> 4);
+#pragma unroll
+                        for (int k = 0; k < BK / 16; ++k) tc_mma_bf16(tm_d, ad + k * a_step, bd + k * b_step, idesc, !first || (term | k) != 0);
+                    }
                     tc_commit(&empty_bar[s]);
+                    if (last) { tc_commit(&acc_full[acc]); ++n_acc; }
                 }
-                if (ok) tc_commit(&acc_full[acc]);
-                ++n_acc;
             }
             if (!ok) {   // given up: the products in flight still read it
                 int late = 0;
@@ -779,46 +783,78 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
         }
     } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;   // tensor-memory lane quadrant; which 128 columns
-        const int et = threadIdx.x - 64;                  // 0..255
+        const int q = warp & 3, group = (warp - 2) >> 2;   // tensor-memory lane quadrant; which columns of the tile
+        const int et = threadIdx.x - 64;                   // 0 .. EPI - 1
         const int row_in_tile = q * 32 + lane;
-        uint32_t n_acc = 0;
+        const int width = group_cols(p.tn, S::GROUPS);
+        const int my0 = group * width;                     // first column of this warp's, in the tile
+        uint32_t n_acc = 0, n_tile = 0;
         bool ok = true;
-        for (long long u = blockIdx.x; u < n_units; u += gridDim.x) {
+        for (long long u = blockIdx.x; u < n_units; u += gridDim.x, ++n_tile) {
             const Unit t = unit_of<MODE>(p, n_rows, u);
-            const uint32_t acc = n_acc & 1u;
-            const uint32_t taddr = tmem_base + acc * LT_N + half * 128 + ((uint32_t)(q * 32) << 16);
+            const uint32_t lanes = tmem_base + my0 + ((uint32_t)(q * 32) << 16);
             const int row = t.mt * BM + row_in_tile;
+            float* bias = s_bias[n_tile & 1];
             if (MODE != PRODUCTS) {
-                const int v = p.v0 + t.nt * LT_N + et;     // outputs behind the last one: probability zero
-                s_bias[acc][et] = v < p.n_out ? (p.bias ? p.bias[v] : 0.f) : -CUDART_INF_F;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (et < p.tn) {
+                    const int v = p.v0 + t.nt * p.tn + et;     // outputs behind the last one: probability zero
+                    bias[et] = v < p.n_out ? (p.bias ? p.bias[v] : 0.f) : -CUDART_INF_F;
+                }
+                __syncwarp();
+                asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
             }
             // (a warp that gives up goes on without waiting: the others still meet it at the barriers)
-            if (t.nk > 0) {
+            // fp32: an accumulator takes one K block, whose sum is added up here.  (Tensor cores cut where they add; over a long K that
+            // is an error of 2^-25 an addition, all one way: 5e-6 of dW over 20 000 rows.)
+            float sums[KIND == F32 ? S::CHUNKS * 32 : 1];
+            uint32_t taddr = lanes;
+            if constexpr (KIND == F32) {
+#pragma unroll
+                for (int i = 0; i < S::CHUNKS * 32; ++i) sums[i] = 0.f;
+                for (int i = 0; i < t.nk; ++i, ++n_acc) {
+                    const uint32_t acc = n_acc & 1u;
+                    ok = ok && mbar_wait_warp(&acc_full[acc], (n_acc >> 1) & 1u, &abort_flag);
+                    __syncwarp();
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 0; c < S::CHUNKS; ++c) {
+                        float v[32];
+                        tmem_ld32(lanes + acc * TN + c * 32, v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) sums[c * 32 + e] += v[e];
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+                }
+            } else if (t.nk > 0) {
+                const uint32_t acc = n_acc & 1u;
                 ok = ok && mbar_wait_warp(&acc_full[acc], (n_acc >> 1) & 1u, &abort_flag);
+                __syncwarp();
                 tc_fence_after();
+                taddr = lanes + acc * TN;
             }
-            const int col = p.v0 + t.nt * LT_N + half * 128;
-            if (!ok) {
-            } else if (MODE == FORWARD) {
-                const int n_cols = min(128, p.n_out - col);
-                if (n_cols > 0) forward_row<LIST>(p, taddr, s_bias[acc] + half * 128, col, n_cols, row, n_rows, t.nt * 2 + half);
-            } else if (MODE == LOGITS) {
-                logits_row<LIST, P>(p, taddr, s_bias[acc] + half * 128, col, t.nt * LT_N + half * 128, row, n_rows, s_db[half * 4 + q]);
-            } else {
-                product_row<P == 3>(p, t, taddr, half, row_in_tile, n_rows, t.nk == 0);
+            if (ok && my0 < p.tn) {
+                if constexpr (MODE == FORWARD) {
+                    const int col = t.nt * p.tn + my0, n_cols = min(width, p.n_out - col);
+                    if (n_cols > 0) forward_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, col, n_cols, row, n_rows, col / width);
+                } else if constexpr (MODE == LOGITS) {
+                    logits_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, t.nt * p.tn + my0, width, row, n_rows, &s_db[q][my0]);
+                } else {
+                    product_row<KIND, S::CHUNKS>(p, t, taddr, sums, t.nt * p.tn + my0, row_in_tile, n_rows, t.nk == 0);
+                }
             }
-            if (t.nk > 0) {
+            if (KIND != F32 && t.nk > 0) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&acc_empty[acc]);
+                if (lane == 0) mbar_arrive(&acc_empty[n_acc & 1u]);
                 ++n_acc;
             }
             if (MODE == LOGITS && p.dbp) {
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                const float* d = &s_db[et >> 7 << 2][et & 127];
-                p.dbp[(size_t)t.mt * p.ldg + t.nt * LT_N + et] = (d[0] + d[128]) + (d[256] + d[384]);
+                __syncwarp();
+                asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
+                const int c = t.nt * p.tn + et;
+                if (et < p.tn && c < p.cols) p.dbp[(size_t)t.mt * p.ldg + c] = (s_db[0][et] + s_db[1][et]) + (s_db[2][et] + s_db[3][et]);
             }
         }
     }
@@ -928,6 +964,78 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const LossCtrl* ctrl, co
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
+// Columns of the tiles of logits.  Narrow ones where wide ones leave SMs idle: the time goes by the CTA with the most tiles, a
+// tile's by its columns and (its rows are loaded all the same) by 64 more.
+static int tile_cols(int row_tiles, int cols, int most) {
+    int best = most;
+    long long least = 0;
+    for (int tn = most; tn >= 64; tn /= 2) {
+        const long long time = (((long long)row_tiles * cdiv(cols, tn) + kFillCtas - 1) / kFillCtas) * (tn + 64);
+        if (tn == most || time < least) { best = tn; least = time; }
+    }
+    return best;
+}
+
+LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad) {
+    LossLayout L{};
+    const bool f32 = o.dtype == WIND_DT_F32;
+    L.planes = f32 ? 3 : 1;
+    L.g_planes = f32 ? 3 : N <= 256 ? 2 : 1;
+    L.pack_w = f32 || o.H % 8 || o.ldw % 8 || (o.n_out > 1 && o.ldw < o.H) || reinterpret_cast<uintptr_t>(o.w) % 16;
+    L.Hp = up(o.H, 64);
+    L.Npad = up(N, 128);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t at = off; off = align_up(off + bytes); return at; };
+    L.ctrl = take(sizeof(LossCtrl));
+    const size_t np = (size_t)L.Npad;
+    const int most = f32 ? Shape<FORWARD, F32>::TN : Shape<FORWARD, BF16>::TN;
+    L.counts = take(N > ROWS_COUNTED ? 4 * (size_t)cdiv(N, ROWS_COUNTED) : 0);
+    L.mark = take(K ? np : 0);
+    L.src = take(4 * np);
+    L.target = take(K ? 0 : 4 * np);
+    L.scale = take(grad ? 4 * np : 0);
+    L.nlse = take(grad ? 4 * np : 0);
+    L.sid = take(4 * (size_t)N * K);
+    L.sq = take(4 * (size_t)N * K);
+    L.ent = take(K ? 4 * np : 0);
+    L.x = take(2 * (size_t)L.planes * np * L.Hp);
+    L.w = take(L.pack_w ? 2 * (size_t)L.planes * o.n_out * L.Hp : 0);
+    if (!grad) {
+        L.tn = tile_cols(L.Npad / BM, o.n_out, most);
+        L.parts = cdiv(o.n_out, group_cols(L.tn, f32 ? Shape<FORWARD, F32>::GROUPS : Shape<FORWARD, BF16>::GROUPS));
+        const size_t parts = (size_t)L.parts;
+        L.pm = take(4 * parts * np);
+        L.ps = take(4 * parts * np);
+        L.pq = take(4 * parts * np);
+    } else {
+        // a piece: as many outputs as keep its g within kLossPieceBytes, 2048 at least (below that the partial sums of dx, read and
+        // written once a piece, cost more than a few per cent of the products)
+        const long long all = up(o.n_out, 256);
+        const long long fit = (long long)(kLossPieceBytes / (2 * (size_t)L.g_planes * (np ? np : 1))) / 256 * 256;
+        L.piece = (int)std::min(all, std::max(2048LL, fit));
+        L.pieces = cdiv(o.n_out, L.piece);
+        L.tn = tile_cols(L.Npad / BM, std::min(o.n_out, L.piece), most);
+        L.tn_products = most;
+        const int ht = cdiv(o.H, L.tn_products), terms = f32 ? 6 : 1;
+        const long long t_dx = (long long)(L.Npad / 128) * ht, t_dw = (long long)cdiv(std::min(o.n_out, L.piece), 128) * ht;
+        const int kb_dx = cdiv(std::min(o.n_out, L.piece), BK), kb_dw = L.Npad / BK;
+        auto parts_of = [&](long long tiles, int kb) {
+            if (tiles <= 0 || tiles >= kFillCtas) return 1;
+            return (int)std::max(1LL, std::min<long long>({kFillCtas / tiles, (long long)kb * terms / 8, (long long)kb}));
+        };
+        L.s_dx = parts_of(t_dx, kb_dx);
+        L.s_dw = parts_of(t_dw, kb_dw);
+        L.slab_dx = L.s_dx > 1 || L.pieces > 1;
+        L.slab_dw = L.s_dw > 1;
+        L.g = take(2 * (size_t)L.g_planes * np * L.piece);
+        L.dbp = take(4 * (np / 128) * L.piece);
+        L.sdx = take(L.slab_dx ? 4 * (size_t)L.s_dx * np * L.Hp : 0);
+        L.sdw = take(L.slab_dw ? 4 * (size_t)L.s_dw * L.piece * L.Hp : 0);
+    }
+    L.total = off;
+    return L;
+}
+
 static PFN_cuTensorMapEncodeTiled g_encode_loss = nullptr;
 static std::mutex g_loss_mutex;
 
@@ -955,20 +1063,21 @@ static cudaError_t loss_map(CUtensorMap* map, const void* base, uint64_t planes,
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-constexpr size_t kLossSmem = (size_t)LT_STAGES * LT_STAGE_BYTES + 1024;
-
 typedef void (*LossKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const LossGemm);
 
-static LossKernel loss_kernel_of(int mode, bool list, int planes) {
-    if (mode == FORWARD) {
-        if (planes == 1) return list ? loss_gemm_kernel<FORWARD, true, 1> : loss_gemm_kernel<FORWARD, false, 1>;
-        return list ? loss_gemm_kernel<FORWARD, true, 3> : loss_gemm_kernel<FORWARD, false, 3>;
+template <int MODE, int KIND>
+static LossKernel loss_kernel_of(bool list) {
+    return list && MODE != PRODUCTS ? loss_gemm_kernel<MODE, MODE != PRODUCTS, KIND> : loss_gemm_kernel<MODE, false, KIND>;
+}
+struct LossLaunch { LossKernel kernel; int threads, smem; };
+template <int MODE>
+static LossLaunch loss_launch_of(bool list, int kind) {
+    if (kind == F32) return {loss_kernel_of<MODE, F32>(list), Shape<MODE, F32>::THREADS, Shape<MODE, F32>::SMEM};
+    if (MODE != FORWARD && kind == BF16_FINE) {
+        constexpr int M = MODE == FORWARD ? LOGITS : MODE;
+        return {loss_kernel_of<M, BF16_FINE>(list), Shape<M, BF16_FINE>::THREADS, Shape<M, BF16_FINE>::SMEM};
     }
-    if (mode == LOGITS) {
-        if (planes == 1) return list ? loss_gemm_kernel<LOGITS, true, 1> : loss_gemm_kernel<LOGITS, false, 1>;
-        return list ? loss_gemm_kernel<LOGITS, true, 3> : loss_gemm_kernel<LOGITS, false, 3>;
-    }
-    return planes == 1 ? loss_gemm_kernel<PRODUCTS, false, 1> : loss_gemm_kernel<PRODUCTS, false, 3>;
+    return {loss_kernel_of<MODE, BF16>(list), Shape<MODE, BF16>::THREADS, Shape<MODE, BF16>::SMEM};
 }
 
 // Shared-memory opt-in of the kernels of this file.
@@ -980,17 +1089,23 @@ static cudaError_t loss_set_attributes() {
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::lock_guard<std::mutex> lock(g_loss_mutex);
     if (done_on[dev]) return cudaSuccess;
-    for (int mode = FORWARD; mode <= PRODUCTS; ++mode)
-        for (int list = 0; list < 2; ++list)
-            for (int planes = 1; planes <= 3; planes += 2)
-                if ((e = cudaFuncSetAttribute(loss_kernel_of(mode, list, planes), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLossSmem)) != cudaSuccess)
-                    return e;
+    for (int list = 0; list < 2; ++list)
+        for (int kind = BF16; kind <= F32; ++kind)
+            for (const LossLaunch& l : {loss_launch_of<FORWARD>(list, kind), loss_launch_of<LOGITS>(list, kind), loss_launch_of<PRODUCTS>(list, kind)})
+                if ((e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, l.smem)) != cudaSuccess) return e;
     done_on[dev] = true;
     return cudaSuccess;
 }
 
-static bool vec_rows(const void* p, int64_t ld, int H, bool f32) {   // 16-byte accesses of rows of H elements
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % (f32 ? 4 : 8) == 0 && H % 8 == 0;
+static int vec_rows(const void* p, int64_t ld, int H, bool f32) {   // accesses of rows of H elements: 0 single, 1 of 16 bytes, 2 of 32
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (f32 ? 4 : 2));
+    return H % 8 || at % 16 ? 0 : at % 32 ? 1 : 2;
+}
+
+static cudaError_t launch_gemm(const LossLaunch& l, long long units, int sms, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& a2,
+                               const CUtensorMap& b2, const LossGemm& p, cudaStream_t stream) {
+    l.kernel<<<(int)std::min<long long>(units, sms), l.threads, l.smem, stream>>>(a, b, a2, b2, p);
+    return cudaGetLastError();
 }
 
 cudaError_t loss_run(const LossCall& c) {
@@ -1063,22 +1178,21 @@ cudaError_t loss_run(const LossCall& c) {
     p.ctrl = ctrl;
     p.n_out = c.o.n_out; p.H = c.o.H; p.Hp = L.Hp; p.Npad = L.Npad; p.K = c.K;
     p.kb = L.Hp / BK;
+    p.tn = L.tn;
     p.rtau = 1.f / c.tau;
     p.bias = c.o.b;
     p.src = r.src; p.target = r.target_c; p.sid = r.sid; p.sq = r.sq;
     CUtensorMap map_x, map_w, map_w64, map_x64, map_g, map_g64;
     if ((e = loss_map(&map_x, r.xc, L.planes, L.Npad, L.Hp, L.Hp, BM)) != cudaSuccess) return e;
-    if ((e = loss_map(&map_w, w, L.planes, c.o.n_out, w_cols, ldw, LT_N)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_w, w, L.planes, c.o.n_out, w_cols, ldw, L.tn)) != cudaSuccess) return e;
     const int row_tiles = L.Npad / BM;
     if (!c.grad) {
-        p.v0 = 0; p.cols = c.o.n_out; p.n_vt = cdiv(c.o.n_out, LT_N);
+        p.v0 = 0; p.cols = c.o.n_out; p.n_vt = cdiv(c.o.n_out, L.tn);
         p.pm = reinterpret_cast<float*>(c.ws + L.pm);
         p.ps = reinterpret_cast<float*>(c.ws + L.ps);
         p.pq = reinterpret_cast<float*>(c.ws + L.pq);
-        const int grid = (int)std::min<long long>((long long)row_tiles * p.n_vt, sms);
-        loss_kernel_of(FORWARD, c.K > 0, L.planes)<<<grid, LT_THREADS, kLossSmem, c.stream>>>(map_x, map_w, map_x, map_w, p);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        loss_combine_kernel<<<cdiv(c.N, 8), 256, 0, c.stream>>>(ctrl, r.src, p.pm, p.ps, p.pq, cdiv(c.o.n_out, 128), L.Npad,
+        if ((e = launch_gemm(loss_launch_of<FORWARD>(c.K > 0, L.planes), (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
+        loss_combine_kernel<<<cdiv(c.N, 8), 256, 0, c.stream>>>(ctrl, r.src, p.pm, p.ps, p.pq, L.parts, L.Npad,
                                                                   c.K ? r.ent : nullptr, c.tau, c.loss, c.lse_out);
         return cudaGetLastError();
     }
@@ -1087,34 +1201,32 @@ cudaError_t loss_run(const LossCall& c) {
     p.g = reinterpret_cast<__nv_bfloat16*>(c.ws + L.g);
     p.ldg = L.piece; p.g_plane = (size_t)L.Npad * L.piece;
     p.dbp = c.db ? reinterpret_cast<float*>(c.ws + L.dbp) : nullptr;
-    p.ht = cdiv(c.o.H, LT_N); p.s_dx = L.s_dx; p.s_dw = L.s_dw;
+    p.ht = cdiv(c.o.H, L.tn_products); p.s_dx = L.s_dx; p.s_dw = L.s_dw;
     p.sdx = L.slab_dx ? reinterpret_cast<float*>(c.ws + L.sdx) : nullptr;
     p.sdw = L.slab_dw ? reinterpret_cast<float*>(c.ws + L.sdw) : nullptr;
     p.slab_rows_dw = L.piece;
     p.dx = c.dx; p.lddx = c.lddx; p.want_dx = c.dx != nullptr; p.dx_vec = vec_rows(c.dx, c.lddx, c.o.H, f32);
     p.dw = c.dw; p.lddw = c.lddw; p.want_dw = c.dw != nullptr; p.dw_vec = vec_rows(c.dw, c.lddw, c.o.H, f32);
-    if ((e = loss_map(&map_g, p.g, L.planes, L.Npad, L.piece, L.piece, BM)) != cudaSuccess) return e;
-    if ((e = loss_map(&map_g64, p.g, L.planes, L.Npad, L.piece, L.piece, 64)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_g, p.g, L.g_planes, L.Npad, L.piece, L.piece, BM)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_g64, p.g, L.g_planes, L.Npad, L.piece, L.piece, 64)) != cudaSuccess) return e;
     if ((e = loss_map(&map_x64, r.xc, L.planes, L.Npad, L.Hp, L.Hp, 64)) != cudaSuccess) return e;
     if ((e = loss_map(&map_w64, w, L.planes, c.o.n_out, w_cols, ldw, 64)) != cudaSuccess) return e;
     const int sum_blocks = 8 * sms;
     for (int piece = 0; piece < L.pieces; ++piece) {
         p.v0 = piece * L.piece;
         p.cols = std::min(L.piece, c.o.n_out - p.v0);
-        p.n_vt = cdiv(p.cols, LT_N);
+        p.tn = L.tn;
+        p.n_vt = cdiv(p.cols, L.tn);
         p.add_dx = piece > 0;
-        int grid = (int)std::min<long long>((long long)row_tiles * p.n_vt, sms);
-        loss_kernel_of(LOGITS, c.K > 0, L.planes)<<<grid, LT_THREADS, kLossSmem, c.stream>>>(map_x, map_w, map_x, map_w, p);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if ((e = launch_gemm(loss_launch_of<LOGITS>(c.K > 0, L.g_planes), (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
         if (c.db) {
             loss_bias_kernel<<<cdiv(p.cols, 32), 256, 0, c.stream>>>(ctrl, p.dbp, L.piece, p.cols, c.db + p.v0);
             if ((e = cudaGetLastError()) != cudaSuccess) return e;
         }
         if (!c.dx && !c.dw) continue;
+        p.tn = L.tn_products;
         const long long units = (c.dx ? (long long)L.s_dx * row_tiles * p.ht : 0) + (c.dw ? (long long)L.s_dw * cdiv(p.cols, BM) * p.ht : 0);
-        grid = (int)std::min<long long>(units, sms);
-        loss_kernel_of(PRODUCTS, false, L.planes)<<<grid, LT_THREADS, kLossSmem, c.stream>>>(map_g, map_w64, map_g64, map_x64, p);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if ((e = launch_gemm(loss_launch_of<PRODUCTS>(false, L.g_planes), units, sms, map_g, map_w64, map_g64, map_x64, p, c.stream)) != cudaSuccess) return e;
         if (c.dw && L.slab_dw) {
             void* out = static_cast<uint8_t*>(c.dw) + (size_t)p.v0 * c.lddw * es;
             if (f32) loss_sum_kernel<true><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdw, L.s_dw, L.piece, p.cols, c.o.H, L.Hp, nullptr, out, c.lddw, p.dw_vec);
