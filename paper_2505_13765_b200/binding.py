@@ -583,41 +583,111 @@ def alloc_loss_workspace(weight, N: int, K: int = 0, grad: bool = False):
     return torch.empty(n + 256, dtype=torch.uint8, device=weight.device)
 
 
-def _loss_call(name: str, x, weight, bias, rows, forward, backward, workspace, stream, check: bool) -> int:
-    """rows: (target,) or (ids, teacher, tau); forward: (loss, lse) or None; backward: (lse, dloss, dx, dw, db) or None."""
-    torch = _torch()
-    o = _output_layer(weight, bias)
-    dev, dt, f32, i32 = weight.device, weight.dtype, torch.float32, torch.int32
+def _ready():
+    """torch, once it has been seen to have a device (asking costs a third of a small call)."""
+    global _torch_ready
+    if _torch_ready is None:
+        _torch_ready = _torch()
+    return _torch_ready
+
+
+_torch_ready = None
+
+
+def _check_loss_call(x, weight, bias, rows, forward, backward, workspace, stream) -> None:
+    """Raises ValueError with what is wrong with a call (the calls themselves only find out whether something is)."""
+    torch = _ready()
+    f32, i32 = torch.float32, torch.int32
+    _output_layer(weight, bias)
+    dev, dt = weight.device, weight.dtype
     _need(dev.type == "cuda", "weight: on a CUDA device")
+    n_out, H = weight.shape
     _need(x.dim() == 2, "x: a matrix [N, H]")
-    N, H, n_out = x.shape[0], o.H, o.n_out
-    args = [C.byref(o), x.data_ptr(), _rows(x, "x", (N, H), dt, dev)]
+    N = x.shape[0]
+    _rows(x, "x", (N, H), dt, dev)
+    for t, name in zip(rows, ("target",) if len(rows) == 1 else ("ids", "teacher", "tau")):
+        _need(t is not None, f"{name}: not given")
+    _need(all(t is not None for t in forward or backward[:1]), "loss, lse: not given")
     if len(rows) == 1:
-        args += [_vector(rows[0], "target", (N,), i32, dev), N]
+        _vector(rows[0], "target", (N,), i32, dev)
     else:
-        ids, teacher, tau = rows
-        _need(ids.dim() == 2, "ids: a matrix [N, K]")
-        K = ids.shape[1]
-        args += [_vector(ids, "ids", (N, K), i32, dev), _vector(teacher, "teacher", (N, K), f32, dev), N, K, float(tau)]
-    if forward:
-        args += [_vector(forward[0], "loss", (N,), f32, dev), _vector(forward[1], "lse", (N,), f32, dev)]
+        _need(rows[0].dim() == 2, "ids: a matrix [N, K]")
+        K = rows[0].shape[1]
+        _vector(rows[0], "ids", (N, K), i32, dev)
+        _vector(rows[1], "teacher", (N, K), f32, dev)
+    if forward is not None:
+        _vector(forward[0], "loss", (N,), f32, dev)
+        _vector(forward[1], "lse", (N,), f32, dev)
     else:
         lse, dloss, dx, dw, db = backward
-        args += [_vector(lse, "lse", (N,), f32, dev), _vector(dloss, "dloss", (N,), f32, dev)]
-        for t, n, shape in ((dx, "dx", (N, H)), (dw, "dw", (n_out, H))):
-            args += [0, 0] if t is None else [t.data_ptr(), _rows(t, n, shape, dt, dev)]
-        args += [_vector(db, "db", (n_out,), f32, dev)]
+        _vector(lse, "lse", (N,), f32, dev)
+        _vector(dloss, "dloss", (N,), f32, dev)
+        if dx is not None:
+            _rows(dx, "dx", (N, H), dt, dev)
+        if dw is not None:
+            _rows(dw, "dw", (n_out, H), dt, dev)
+        _vector(db, "db", (n_out,), f32, dev)
+    _need(workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace: contiguous bytes")
     _need(workspace.device == dev, f"workspace: on {workspace.device}, not {dev}")
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    _need(stream.device == dev, f"stream: on {stream.device}, not {dev}")
-    args += [_ws_ptr(workspace), _ws_bytes(workspace), int(stream.cuda_stream)]
-    L = load_library()
-    if torch.cuda.current_device() == dev.index:
-        st = getattr(L, name)(*args)
+    _need(stream is None or stream.device == dev, f"stream: not on {dev}")
+
+
+def _loss_call(name: str, x, weight, bias, rows, forward, backward, workspace, stream, check: bool) -> int:
+    """rows: (target,) or (ids, teacher, tau); forward: (loss, lse) or None; backward: (lse, dloss, dx, dw, db) or None."""
+    torch = _ready()
+    f32, i32, dt, dev = torch.float32, torch.int32, weight.dtype, weight.get_device()
+    ok = True
+
+    def matrix(t, shape):
+        nonlocal ok
+        d, s = t.stride() if t.dim() == 2 else (0, 0)
+        ok = ok and t.shape == shape and t.dtype is dt and t.get_device() == dev and (s == 1 or shape[1] == 1 or not shape[0])
+        return (t.data_ptr(), d if shape[0] > 1 else shape[1]) if ok else (0, 0)
+
+    def vector(t, shape, dtype, needed=True):
+        nonlocal ok
+        if t is None:
+            ok = ok and not needed
+            return None
+        ok = ok and t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()
+        return t.data_ptr()
+
+    if weight.dim() != 2 or x.dim() != 2 or dev < 0 or not (dt is torch.bfloat16 or dt is f32):
+        ok, n_out, H, N = False, 0, 0, 0
+    else:
+        (n_out, H), N = weight.shape, x.shape[0]
+    w, ldw = matrix(weight, (n_out, H))
+    o = wind_output_t(n_out, H, WIND_DT_F32 if dt is f32 else WIND_DT_BF16, 0, w, ldw, vector(bias, (n_out,), f32, False))
+    args = [C.byref(o), *matrix(x, (N, H))]
+    if len(rows) == 1:
+        args += (vector(rows[0], (N,), i32), N)
+    else:
+        ids, teacher, tau = rows
+        K = ids.shape[1] if ids.dim() == 2 else -1
+        args += (vector(ids, (N, K), i32), vector(teacher, (N, K), f32), N, K, tau)
+    if forward is not None:
+        args += (vector(forward[0], (N,), f32), vector(forward[1], (N,), f32))
+    else:
+        lse, dloss, dx, dw, db = backward
+        args += (vector(lse, (N,), f32), vector(dloss, (N,), f32, False))
+        args += (None, 0) if dx is None else matrix(dx, (N, H))
+        args += (None, 0) if dw is None else matrix(dw, (n_out, H))
+        args.append(vector(db, (n_out,), f32, False))
+    at = workspace.data_ptr()
+    up = -at % 256
+    ok = ok and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == dev
+    ok = ok and (stream is None or stream.device_index == dev)
+    if not ok:
+        _check_loss_call(x, weight, bias, rows, forward, backward, workspace, stream)
+        raise ValueError("arguments of the wrong kind")
+    raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    args += (at + up, workspace.numel() - up, raw)
+    f = getattr(load_library(), name)
+    if torch._C._cuda_getDevice() == dev:
+        st = f(*args)
     else:
         with torch.cuda.device(dev):
-            st = getattr(L, name)(*args)
+            st = f(*args)
     if st != WIND_OK:
         raise WindError(st)
     return wind_loss_status(workspace, stream) if check else st
@@ -650,7 +720,7 @@ def wind_distill_loss_grad(x, weight, bias, ids, teacher, tau: float, lse, dloss
 
 def wind_loss_status(workspace, stream=None, check: bool = True) -> int:
     """Waits for the stream; the status of the last loss or gradient call that used `workspace`."""
-    torch = _torch()
+    torch = _ready()
     if stream is None:
         stream = torch.cuda.current_stream(workspace.device)
     with torch.cuda.device(workspace.device):

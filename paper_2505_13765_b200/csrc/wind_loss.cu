@@ -8,8 +8,8 @@
 // Both losses are one computation: a softmax over all outputs against a target distribution of K >= 1 entries.
 //
 //     loss_list     the teacher's entries of a row to probabilities, sorted by label
-//     loss_gather   rows that count, one behind the other, as tensor-core operands: padding costs nothing from here on
-//     loss_pack     W as tensor-core operands, where it is not one already
+//     loss_gather   rows that count, one behind the other, as tensor-core operands: padding costs nothing from here on; W as a
+//                   tensor-core operand, where it is not one already
 //     loss_gemm     FORWARD   128 x 256 tiles of logits on the tensor cores; of each tile's row only (maximum, sum of exponentials,
 //                             sum of q z) leave the chip
 //                   LOGITS    the same tiles again, turned into g, for a piece of the outputs
@@ -59,6 +59,9 @@ enum Mark : uint8_t { ROW_NONE = 0, ROW_COUNTS = 1, ROW_BAD = 2 };   // BAD: a l
 struct RowsParams {
     LossCtrl* ctrl;
     int N, n_out, K, H, Hp, Npad, x_vec, grad;
+    int row_blocks;            // blocks of loss_gather that take rows; those behind them lay W out
+    const void* w; int64_t ldw; int w_vec; __nv_bfloat16* wc;
+    float* db;                 // where its only writers are the tiles of logits
     int counted;               // counts[] holds the rows that count, of every ROWS_COUNTED rows
     int per_block;             // rows of a block of loss_gather, a multiple of 8
     float tau;
@@ -82,6 +85,8 @@ __device__ __forceinline__ uint8_t row_mark(const RowsParams& p, int r) {
 // before it: K^2 / 32 comparisons a lane.
 __global__ void __launch_bounds__(256) loss_list_kernel(const RowsParams p) {
     __shared__ int32_t s_ids[8][kLossMaxK];
+    let_next_start();
+    wait_for_previous();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r = blockIdx.x * 8 + warp;
     if (r >= p.N) return;
@@ -139,6 +144,8 @@ constexpr int COUNTED_BAD = 1 << 30;   // a row among them is none
 // Rows that count, of every ROWS_COUNTED rows: only for calls so long that the blocks of loss_gather should not count them all.
 __global__ void __launch_bounds__(256) loss_count_kernel(const RowsParams p) {
     __shared__ int s_count;
+    let_next_start();
+    wait_for_previous();
     if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
     int n = 0, bad = 0;
@@ -232,6 +239,21 @@ __device__ __forceinline__ void store_one(void* row, int c, float v) {
     else static_cast<__nv_bfloat16*>(row)[c] = __float2bfloat16_rn(v);
 }
 
+// W as tensor-core operands, by `blocks` blocks.
+template <bool F32>
+__device__ __forceinline__ void pack_w(const RowsParams& p, int block, int blocks) {
+    const size_t plane = (size_t)p.n_out * p.Hp;
+    const int per_row = p.Hp / 8;
+    const long long all = (long long)p.n_out * per_row;
+#pragma unroll 2
+    for (long long i = (long long)block * 256 + threadIdx.x; i < all; i += (long long)blocks * 256) {
+        const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * 8;
+        float v[8];
+        load8<F32>(static_cast<const uint8_t*>(p.w) + (size_t)r * p.ldw * (F32 ? 4 : 2), c, p.H, p.w_vec, v);
+        store8<F32>(p.wc + (size_t)r * p.Hp + c, plane, v);
+    }
+}
+
 // A block takes per_block rows, a warp a row at a time.  Where its first row that counts goes is the number of such rows before it,
 // which every block finds out for itself: reading up to ROWS_COUNTED marks from L2 is quicker than another launch.
 template <bool F32>
@@ -239,6 +261,12 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
     __shared__ int s_before[8], s_pos[256];
     __shared__ uint32_t s_ballot[8];
     __shared__ uint8_t s_mark[256];
+    let_next_start();
+    wait_for_previous();
+    if ((int)blockIdx.x >= p.row_blocks) {
+        pack_w<F32>(p, blockIdx.x - p.row_blocks, gridDim.x - p.row_blocks);
+        return;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r0 = blockIdx.x * p.per_block, r1 = min(r0 + p.per_block, p.N);
     int before = 0, first = 0;
@@ -303,7 +331,7 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
             }
         }
     }
-    if (blockIdx.x == gridDim.x - 1) {
+    if ((int)blockIdx.x == p.row_blocks - 1) {
         // the last row tile is full of zeros behind the last row
         if (threadIdx.x == 0) {   // (this block has seen every mark)
             p.ctrl->status = bad ? WIND_ERR_INVALID_ARG : WIND_OK;
@@ -312,19 +340,8 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
         const float zero[8] = {};
         for (int j = total + warp; j < (total + 127) / 128 * 128; j += 8)
             for (int c = lane * 8; c < p.Hp; c += 256) store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, zero);
-    }
-}
-
-template <bool F32>
-__global__ void __launch_bounds__(256) loss_pack_kernel(const void* w, int64_t ldw, int rows, int H, int Hp, int vec, __nv_bfloat16* out) {
-    const size_t plane = (size_t)rows * Hp;
-    const int per_row = Hp / 8;
-    const long long all = (long long)rows * per_row;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * 8;
-        float v[8];
-        load8<F32>(static_cast<const uint8_t*>(w) + (size_t)r * ldw * (F32 ? 4 : 2), c, H, vec, v);
-        store8<F32>(out + (size_t)r * Hp + c, plane, v);
+        if (p.db && total == 0)      // (no tile of logits is there to write it)
+            for (int v = threadIdx.x; v < p.n_out; v += 256) p.db[v] = 0.f;
     }
 }
 
@@ -340,6 +357,9 @@ struct LossGemm {
     int n_out, H, Hp, Npad, K;
     int kb;                       // K blocks of the logits
     int tn;                       // columns of a tile: 64, 128 or 256
+    int stages, stage_bytes;      // the ring of K blocks (see ring_of)
+    int a_rows;                   // rows that a fetch of x, or of g for dx, brings; b_bytes: what lies between the parts of B
+    int b_bytes;
     int v0, cols, n_vt;           // this piece's first output, its outputs (to n_out at most) and tiles
     float rtau;                   // 1 / tau
     const float* bias;
@@ -361,18 +381,17 @@ struct Shape {
     static constexpr int TN = KIND == F32 ? 128 : 256;                                       // most columns of a tile (BM = 128 rows)
     static constexpr int A_PARTS = KIND == F32 ? 3 : (KIND == BF16_FINE && MODE == PRODUCTS ? 2 : 1), B_PARTS = KIND == F32 ? 3 : 1;
     static constexpr int TERMS = KIND == F32 ? 6 : A_PARTS;
-    static constexpr int B_BYTES = TN * BK * 2;
-    static constexpr int STAGE_BYTES = A_PARTS * A_STAGE_BYTES + B_PARTS * B_BYTES;
-    static constexpr int STAGES = 196608 / STAGE_BYTES;                                      // 4, 3 (fine) or 2 (fp32)
+    static constexpr int WORST = A_PARTS * A_STAGE_BYTES + B_PARTS * TN * BK * 2;            // bytes of a full stage
     // Groups of four epilogue warps (one per tensor-memory lane quadrant), each with its columns of a tile.  The gradient's share of
     // logits takes more of the ALUs than the softmax's sums do: 16 warps hide more of it than 8.
     static constexpr int GROUPS = MODE == LOGITS && KIND != F32 ? 4 : 2;
     static constexpr int EPI = 128 * GROUPS, THREADS = 64 + EPI, CHUNKS = TN / GROUPS / 32;
-    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
     // Part products, smallest first: the parts of A and B of each (fp32: 20 02 11 10 01 00; fine: 10 00).
     static __device__ __forceinline__ constexpr int a_part(int t) { return KIND == F32 ? (0x001102 >> (4 * t)) & 3 : TERMS - 1 - t; }
     static __device__ __forceinline__ constexpr int b_part(int t) { return KIND == F32 ? (0x010120 >> (4 * t)) & 3 : 0; }
 };
+constexpr int kRingBytes = 196608 + A_STAGE_BYTES;   // 4 full stages of bf16, 3 of fine, 2 of fp32, and what a short A reads behind its last
+constexpr int kMaxStages = 16;
 __host__ __device__ constexpr int group_cols(int tn, int groups) { return tn / groups > 32 ? tn / groups : 32; }
 
 // K-major tiles as in smem_desc_sw128.  MN-major ones: panels of 64 (M or N) x 64 (K) bf16, a K row of a panel being 128 bytes: 8 K rows
@@ -677,9 +696,9 @@ __global__ void __launch_bounds__((Shape<MODE, KIND>::THREADS), 1)
 loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a2,
                  const __grid_constant__ CUtensorMap map_b2, const LossGemm p) {
     using S = Shape<MODE, KIND>;
-    constexpr int TN = S::TN, EPI = S::EPI, STAGES = S::STAGES, A_PARTS = S::A_PARTS, B_PARTS = S::B_PARTS;
+    constexpr int TN = S::TN, EPI = S::EPI, A_PARTS = S::A_PARTS, B_PARTS = S::B_PARTS;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], acc_full[2], acc_empty[2], drain_bar;
+    __shared__ uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], acc_full[2], acc_empty[2], drain_bar;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ float s_bias[2][TN];
@@ -690,7 +709,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
+        for (int s = 0; s < p.stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], EPI / 32); }
         mbar_init(&drain_bar, 1);
         fence_barrier_init();
@@ -702,49 +721,58 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = tmem_slot;
+    let_next_start();
+    wait_for_previous();
     const int n_rows = p.ctrl->n_rows;
     const long long n_units = count_units<MODE>(p, n_rows);
 
     if (warp == 0) {
         if (elect_one()) {
-            uint32_t it = 0;
+            int s = 0;
+            uint32_t turn = 0;       // of the ring: stage s is used for the (turn + 1)-th time
             bool ok = true;
             for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 const Unit t = unit_of<MODE>(p, n_rows, u);
                 const int panels = (unit_cols<MODE>(p, t) + 63) / 64;
-                const uint32_t b_bytes = MODE == PRODUCTS ? panels * PANEL_BYTES : p.tn * BK * 2;
-                for (int kb = t.k0; kb < t.k0 + t.nk; ++kb, ++it) {
-                    const int s = it % STAGES;
-                    if (!mbar_wait(&empty_bar[s], ((it / STAGES) & 1) ^ 1, &abort_flag)) { ok = false; break; }
-                    uint8_t* a = smem + (size_t)s * S::STAGE_BYTES;
-                    uint8_t* b = a + A_PARTS * A_STAGE_BYTES;
-                    mbar_expect_tx(&full_bar[s], A_PARTS * A_STAGE_BYTES + B_PARTS * b_bytes);
+                const int a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2;
+                const uint32_t bytes = A_PARTS * a_part + B_PARTS * (MODE == PRODUCTS ? panels * PANEL_BYTES : p.tn * BK * 2);
+                for (int kb = t.k0; kb < t.k0 + t.nk; ++kb) {
+                    if (!mbar_wait(&empty_bar[s], (turn & 1) ^ 1, &abort_flag)) { ok = false; break; }
+                    uint8_t* a = smem + (size_t)s * p.stage_bytes;
+                    uint8_t* b = a + A_PARTS * a_part;
+                    uint64_t* full = &full_bar[s];
+                    mbar_expect_tx(full, bytes);
                     if (MODE != PRODUCTS) {
-                        for (int i = 0; i < A_PARTS; ++i) tma_load_3d(a + i * A_STAGE_BYTES, &map_a, kb * BK, t.mt * BM, i, &full_bar[s]);
-                        for (int i = 0; i < B_PARTS; ++i) tma_load_3d(b + i * S::B_BYTES, &map_b, kb * BK, p.v0 + t.nt * p.tn, i, &full_bar[s]);
+                        for (int i = 0; i < A_PARTS; ++i) tma_load_3d(a + i * a_part, &map_a, kb * BK, t.mt * BM, i, full);
+                        for (int i = 0; i < B_PARTS; ++i) tma_load_3d(b + i * p.b_bytes, &map_b, kb * BK, p.v0 + t.nt * p.tn, i, full);
                     } else if (!t.dw) {
-                        for (int i = 0; i < A_PARTS; ++i) tma_load_3d(a + i * A_STAGE_BYTES, &map_a, kb * BK, t.mt * BM, i, &full_bar[s]);
+                        for (int i = 0; i < A_PARTS; ++i) tma_load_3d(a + i * a_part, &map_a, kb * BK, t.mt * BM, i, full);
                         for (int i = 0; i < B_PARTS; ++i)
                             for (int q = 0; q < panels; ++q)
-                                tma_load_3d(b + i * S::B_BYTES + q * PANEL_BYTES, &map_b, t.nt * p.tn + q * 64, p.v0 + kb * BK, i, &full_bar[s]);
+                                tma_load_3d(b + i * p.b_bytes + q * PANEL_BYTES, &map_b, t.nt * p.tn + q * 64, p.v0 + kb * BK, i, full);
                     } else {
                         for (int i = 0; i < A_PARTS; ++i)
                             for (int q = 0; q < 2; ++q)
-                                tma_load_3d(a + i * A_STAGE_BYTES + q * PANEL_BYTES, &map_a2, t.mt * BM + q * 64, kb * BK, i, &full_bar[s]);
+                                tma_load_3d(a + i * a_part + q * PANEL_BYTES, &map_a2, t.mt * BM + q * 64, kb * BK, i, full);
                         for (int i = 0; i < B_PARTS; ++i)
                             for (int q = 0; q < panels; ++q)
-                                tma_load_3d(b + i * S::B_BYTES + q * PANEL_BYTES, &map_b2, t.nt * p.tn + q * 64, kb * BK, i, &full_bar[s]);
+                                tma_load_3d(b + i * p.b_bytes + q * PANEL_BYTES, &map_b2, t.nt * p.tn + q * 64, kb * BK, i, full);
                     }
+                    if (++s == p.stages) { s = 0; ++turn; }
                 }
             }
             if (!ok) {   // given up: the copies in flight still write into this CTA's shared memory
                 int late = 0;
-                for (uint32_t i = it > STAGES ? it - STAGES : 0; i < it; ++i) mbar_wait(&full_bar[i % STAGES], (i / STAGES) & 1, &late);
+                for (int i = 0; i < p.stages; ++i) {
+                    const uint32_t uses = turn + (i < s);        // of stage i
+                    if (uses) mbar_wait(&full_bar[i], (uses - 1) & 1, &late);
+                }
             }
         }
     } else if (warp == 1) {
         if (elect_one()) {
-            uint32_t it = 0, n_acc = 0;
+            int s = 0;
+            uint32_t turn = 0, n_acc = 0;
             bool ok = true;
             for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 const Unit t = unit_of<MODE>(p, n_rows, u);
@@ -753,26 +781,27 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const uint32_t idesc = idesc_bf16(BM, n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                 const uint64_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;   // 16 of K, in units of 16 bytes
                 uint32_t tm_d = 0;
-                for (int i = 0; i < t.nk; ++i, ++it) {
+                const int a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2;
+                for (int i = 0; i < t.nk; ++i) {
                     const uint32_t acc = n_acc & 1u;
                     const bool first = KIND == F32 || i == 0, last = KIND == F32 || i == t.nk - 1;   // of an accumulator
                     if (first) {
                         if (!mbar_wait(&acc_empty[acc], ((n_acc >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
                         tm_d = tmem_base + acc * TN;
                     }
-                    const int s = it % STAGES;
-                    if (!mbar_wait(&full_bar[s], (it / STAGES) & 1, &abort_flag)) { ok = false; break; }
+                    if (!mbar_wait(&full_bar[s], turn & 1, &abort_flag)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t a_addr = smem_u32(smem + (size_t)s * S::STAGE_BYTES), b_addr = a_addr + A_PARTS * A_STAGE_BYTES;
+                    const uint32_t a_addr = smem_u32(smem + (size_t)s * p.stage_bytes), b_addr = a_addr + A_PARTS * a_part;
                     const uint64_t adesc = a_mn ? smem_desc_mn(a_addr) : smem_desc_sw128(a_addr);
                     const uint64_t bdesc = b_mn ? smem_desc_mn(b_addr) : smem_desc_sw128(b_addr);
 #pragma unroll
                     for (int term = 0; term < S::TERMS; ++term) {
-                        const uint64_t ad = adesc + S::a_part(term) * (A_STAGE_BYTES >> 4), bd = bdesc + S::b_part(term) * (S::B_BYTES >> 4);
+                        const uint64_t ad = adesc + S::a_part(term) * (a_part >> 4), bd = bdesc + S::b_part(term) * (p.b_bytes >> 4);
 #pragma unroll
                         for (int k = 0; k < BK / 16; ++k) tc_mma_bf16(tm_d, ad + k * a_step, bd + k * b_step, idesc, !first || (term | k) != 0);
                     }
                     tc_commit(&empty_bar[s]);
+                    if (++s == p.stages) { s = 0; ++turn; }
                     if (last) { tc_commit(&acc_full[acc]); ++n_acc; }
                 }
             }
@@ -876,6 +905,8 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 __global__ void __launch_bounds__(256) loss_combine_kernel(const LossCtrl* ctrl, const int32_t* src, const float* pm, const float* ps, const float* pq,
                                                            int parts, int Npad, const float* ent, float tau, float* loss, float* lse) {
     __shared__ float s_m[32][8], s_s[32][8], s_q[32][8];
+    let_next_start();
+    wait_for_previous();
     const int at_row = threadIdx.x & 7, slice = threadIdx.x >> 3;
     const int j = blockIdx.x * 8 + at_row, n = ctrl->n_rows;
     if ((int)blockIdx.x * 8 >= n) return;
@@ -921,6 +952,8 @@ __global__ void __launch_bounds__(256) loss_combine_kernel(const LossCtrl* ctrl,
 template <bool F32>
 __global__ void __launch_bounds__(256) loss_sum_kernel(const LossCtrl* ctrl, const float* slab, int parts, int slab_rows, int rows, int H, int Hp,
                                                        const int32_t* src, void* out, int64_t ld, int vec) {
+    let_next_start();
+    wait_for_previous();
     if (src) rows = ctrl->n_rows;
     const int per_row = (H + 3) / 4;
     const long long all = (long long)rows * per_row;
@@ -949,6 +982,8 @@ __global__ void __launch_bounds__(256) loss_sum_kernel(const LossCtrl* ctrl, con
 // db of a piece: sums of the row tiles' column sums, 32 outputs x 8 slices a block.
 __global__ void __launch_bounds__(256) loss_bias_kernel(const LossCtrl* ctrl, const float* dbp, int ld, int cols, float* db) {
     __shared__ float s_sum[8][32];
+    let_next_start();
+    wait_for_previous();
     const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     const int tiles = (ctrl->n_rows + BM - 1) / BM;
     float sum = 0.f;
@@ -1069,15 +1104,15 @@ template <int MODE, int KIND>
 static LossKernel loss_kernel_of(bool list) {
     return list && MODE != PRODUCTS ? loss_gemm_kernel<MODE, MODE != PRODUCTS, KIND> : loss_gemm_kernel<MODE, false, KIND>;
 }
-struct LossLaunch { LossKernel kernel; int threads, smem; };
+struct LossLaunch { LossKernel kernel; int threads, a_parts, b_parts; };
 template <int MODE>
 static LossLaunch loss_launch_of(bool list, int kind) {
-    if (kind == F32) return {loss_kernel_of<MODE, F32>(list), Shape<MODE, F32>::THREADS, Shape<MODE, F32>::SMEM};
+    if (kind == F32) return {loss_kernel_of<MODE, F32>(list), Shape<MODE, F32>::THREADS, Shape<MODE, F32>::A_PARTS, Shape<MODE, F32>::B_PARTS};
     if (MODE != FORWARD && kind == BF16_FINE) {
         constexpr int M = MODE == FORWARD ? LOGITS : MODE;
-        return {loss_kernel_of<M, BF16_FINE>(list), Shape<M, BF16_FINE>::THREADS, Shape<M, BF16_FINE>::SMEM};
+        return {loss_kernel_of<M, BF16_FINE>(list), Shape<M, BF16_FINE>::THREADS, Shape<M, BF16_FINE>::A_PARTS, Shape<M, BF16_FINE>::B_PARTS};
     }
-    return {loss_kernel_of<MODE, BF16>(list), Shape<MODE, BF16>::THREADS, Shape<MODE, BF16>::SMEM};
+    return {loss_kernel_of<MODE, BF16>(list), Shape<MODE, BF16>::THREADS, Shape<MODE, BF16>::A_PARTS, Shape<MODE, BF16>::B_PARTS};
 }
 
 // Shared-memory opt-in of the kernels of this file.
@@ -1092,7 +1127,7 @@ static cudaError_t loss_set_attributes() {
     for (int list = 0; list < 2; ++list)
         for (int kind = BF16; kind <= F32; ++kind)
             for (const LossLaunch& l : {loss_launch_of<FORWARD>(list, kind), loss_launch_of<LOGITS>(list, kind), loss_launch_of<PRODUCTS>(list, kind)})
-                if ((e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, l.smem)) != cudaSuccess) return e;
+                if ((e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + 1024)) != cudaSuccess) return e;
     done_on[dev] = true;
     return cudaSuccess;
 }
@@ -1102,10 +1137,30 @@ static int vec_rows(const void* p, int64_t ld, int H, bool f32) {   // accesses 
     return H % 8 || at % 16 ? 0 : at % 32 ? 1 : 2;
 }
 
+// (every kernel here waits for the one before it ahead of its first access to memory)
+template <typename... Params, typename... Args>
+static cudaError_t launch_small(void (*kernel)(Params...), int blocks, cudaStream_t stream, const Args&... args) {
+    static_assert(sizeof...(Params) == sizeof...(Args), "");
+    return [&](Params... typed) {
+        void* list[] = {(void*)&typed...};
+        return launch_overlapped((const void*)kernel, dim3((unsigned)blocks), dim3(256), list, 0, stream);
+    }(args...);
+}
+
+// The ring of K blocks in shared memory.  A stage holds what is fetched: a_rows rows of A (few, where the call has few: the products
+// read 128, and what lies behind the a_rows makes rows of the result that nobody looks at) and a tile's columns of B.  A call of one
+// row has 16 K blocks of 64 columns under way instead of four.
+static void ring_of(LossGemm& p, int a_parts, int b_parts, int a_rows, int tn) {
+    p.a_rows = a_rows;
+    p.b_bytes = tn * BK * 2;
+    p.stage_bytes = a_parts * a_rows * BK * 2 + b_parts * p.b_bytes;
+    p.stages = std::min(kMaxStages, (kRingBytes - A_STAGE_BYTES) / p.stage_bytes);
+}
+
 static cudaError_t launch_gemm(const LossLaunch& l, long long units, int sms, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& a2,
                                const CUtensorMap& b2, const LossGemm& p, cudaStream_t stream) {
-    l.kernel<<<(int)std::min<long long>(units, sms), l.threads, l.smem, stream>>>(a, b, a2, b2, p);
-    return cudaGetLastError();
+    void* args[5] = {(void*)&a, (void*)&b, (void*)&a2, (void*)&b2, (void*)&p};
+    return launch_overlapped((const void*)l.kernel, dim3((unsigned)std::min<long long>(units, sms)), dim3(l.threads), args, kRingBytes + 1024, stream);
 }
 
 cudaError_t loss_run(const LossCall& c) {
@@ -1147,32 +1202,26 @@ cudaError_t loss_run(const LossCall& c) {
     r.xc = reinterpret_cast<__nv_bfloat16*>(c.ws + L.x);
     r.loss = c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.dloss; r.dx = c.dx; r.lddx = c.lddx;
     if (c.K) {
-        loss_list_kernel<<<cdiv(c.N, 8), 256, 0, c.stream>>>(r);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if ((e = launch_small(loss_list_kernel, cdiv(c.N, 8), c.stream, r)) != cudaSuccess) return e;
     }
     r.counted = c.N > ROWS_COUNTED;
     if (r.counted) {
-        loss_count_kernel<<<cdiv(c.N, ROWS_COUNTED), 256, 0, c.stream>>>(r);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if ((e = launch_small(loss_count_kernel, cdiv(c.N, ROWS_COUNTED), c.stream, r)) != cudaSuccess) return e;
     }
     r.per_block = std::min(256, up(cdiv(c.N, 16 * sms), 8));   // a block's warps take one row each while that fills the chip
-    const int row_blocks = cdiv(c.N, r.per_block);
-    if (f32) loss_gather_kernel<true><<<row_blocks, 256, 0, c.stream>>>(r);
-    else loss_gather_kernel<false><<<row_blocks, 256, 0, c.stream>>>(r);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-
+    r.row_blocks = cdiv(c.N, r.per_block);
     const void* w = c.o.w;
     int64_t ldw = c.o.ldw;
-    int w_cols = c.o.H;
+    int w_cols = c.o.H, pack_blocks = 0;
     if (L.pack_w) {
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(c.ws + L.w);
-        const int blocks = (int)std::min<long long>(((long long)c.o.n_out * (L.Hp / 8) + 255) / 256, 8LL * sms);
-        const int vec = vec_rows(c.o.w, c.o.ldw, c.o.H, f32);
-        if (f32) loss_pack_kernel<true><<<blocks, 256, 0, c.stream>>>(w, ldw, c.o.n_out, c.o.H, L.Hp, vec, out);
-        else loss_pack_kernel<false><<<blocks, 256, 0, c.stream>>>(w, ldw, c.o.n_out, c.o.H, L.Hp, vec, out);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        w = out; ldw = L.Hp; w_cols = L.Hp;
+        r.w = w; r.ldw = ldw; r.w_vec = vec_rows(w, ldw, c.o.H, f32);
+        r.wc = reinterpret_cast<__nv_bfloat16*>(c.ws + L.w);
+        pack_blocks = (int)std::min<long long>(((long long)c.o.n_out * (L.Hp / 8) + 255) / 256, 8LL * sms);
+        w = r.wc; ldw = L.Hp; w_cols = L.Hp;
     }
+    const bool one_tile = L.Npad == BM;      // of rows: then the tiles of logits write db themselves
+    if (c.grad && one_tile) r.db = c.db;
+    if ((e = launch_small(f32 ? loss_gather_kernel<true> : loss_gather_kernel<false>, r.row_blocks + pack_blocks, c.stream, r)) != cudaSuccess) return e;
 
     LossGemm p{};
     p.ctrl = ctrl;
@@ -1182,8 +1231,9 @@ cudaError_t loss_run(const LossCall& c) {
     p.rtau = 1.f / c.tau;
     p.bias = c.o.b;
     p.src = r.src; p.target = r.target_c; p.sid = r.sid; p.sq = r.sq;
+    const int few = std::min(BM, up(c.N, 8));    // rows of A that a fetch brings
     CUtensorMap map_x, map_w, map_w64, map_x64, map_g, map_g64;
-    if ((e = loss_map(&map_x, r.xc, L.planes, L.Npad, L.Hp, L.Hp, BM)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_x, r.xc, L.planes, L.Npad, L.Hp, L.Hp, few)) != cudaSuccess) return e;
     if ((e = loss_map(&map_w, w, L.planes, c.o.n_out, w_cols, ldw, L.tn)) != cudaSuccess) return e;
     const int row_tiles = L.Npad / BM;
     if (!c.grad) {
@@ -1191,54 +1241,57 @@ cudaError_t loss_run(const LossCall& c) {
         p.pm = reinterpret_cast<float*>(c.ws + L.pm);
         p.ps = reinterpret_cast<float*>(c.ws + L.ps);
         p.pq = reinterpret_cast<float*>(c.ws + L.pq);
-        if ((e = launch_gemm(loss_launch_of<FORWARD>(c.K > 0, L.planes), (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
-        loss_combine_kernel<<<cdiv(c.N, 8), 256, 0, c.stream>>>(ctrl, r.src, p.pm, p.ps, p.pq, L.parts, L.Npad,
-                                                                  c.K ? r.ent : nullptr, c.tau, c.loss, c.lse_out);
-        return cudaGetLastError();
+        const LossLaunch l = loss_launch_of<FORWARD>(c.K > 0, L.planes);
+        ring_of(p, l.a_parts, l.b_parts, few, L.tn);
+        if ((e = launch_gemm(l, (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
+        return launch_small(loss_combine_kernel, cdiv(c.N, 8), c.stream, ctrl, r.src, p.pm, p.ps, p.pq, L.parts, L.Npad, c.K ? r.ent : nullptr, c.tau,
+                            c.loss, c.lse_out);
     }
 
     p.scale = r.scale_c; p.nlse = r.nlse_c;
     p.g = reinterpret_cast<__nv_bfloat16*>(c.ws + L.g);
     p.ldg = L.piece; p.g_plane = (size_t)L.Npad * L.piece;
-    p.dbp = c.db ? reinterpret_cast<float*>(c.ws + L.dbp) : nullptr;
     p.ht = cdiv(c.o.H, L.tn_products); p.s_dx = L.s_dx; p.s_dw = L.s_dw;
     p.sdx = L.slab_dx ? reinterpret_cast<float*>(c.ws + L.sdx) : nullptr;
     p.sdw = L.slab_dw ? reinterpret_cast<float*>(c.ws + L.sdw) : nullptr;
     p.slab_rows_dw = L.piece;
     p.dx = c.dx; p.lddx = c.lddx; p.want_dx = c.dx != nullptr; p.dx_vec = vec_rows(c.dx, c.lddx, c.o.H, f32);
     p.dw = c.dw; p.lddw = c.lddw; p.want_dw = c.dw != nullptr; p.dw_vec = vec_rows(c.dw, c.lddw, c.o.H, f32);
-    if ((e = loss_map(&map_g, p.g, L.g_planes, L.Npad, L.piece, L.piece, BM)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_g, p.g, L.g_planes, L.Npad, L.piece, L.piece, few)) != cudaSuccess) return e;
     if ((e = loss_map(&map_g64, p.g, L.g_planes, L.Npad, L.piece, L.piece, 64)) != cudaSuccess) return e;
     if ((e = loss_map(&map_x64, r.xc, L.planes, L.Npad, L.Hp, L.Hp, 64)) != cudaSuccess) return e;
     if ((e = loss_map(&map_w64, w, L.planes, c.o.n_out, w_cols, ldw, 64)) != cudaSuccess) return e;
     const int sum_blocks = 8 * sms;
+    const auto sum_kernel = f32 ? loss_sum_kernel<true> : loss_sum_kernel<false>;
     for (int piece = 0; piece < L.pieces; ++piece) {
         p.v0 = piece * L.piece;
         p.cols = std::min(L.piece, c.o.n_out - p.v0);
         p.tn = L.tn;
         p.n_vt = cdiv(p.cols, L.tn);
         p.add_dx = piece > 0;
-        if ((e = launch_gemm(loss_launch_of<LOGITS>(c.K > 0, L.g_planes), (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
-        if (c.db) {
-            loss_bias_kernel<<<cdiv(p.cols, 32), 256, 0, c.stream>>>(ctrl, p.dbp, L.piece, p.cols, c.db + p.v0);
-            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        p.dbp = !c.db ? nullptr : one_tile ? c.db + p.v0 : reinterpret_cast<float*>(c.ws + L.dbp);
+        const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, L.g_planes);
+        ring_of(p, l.a_parts, l.b_parts, few, L.tn);
+        if ((e = launch_gemm(l, (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
+        if (c.db && !one_tile) {
+            if ((e = launch_small(loss_bias_kernel, cdiv(p.cols, 32), c.stream, ctrl, p.dbp, L.piece, p.cols, c.db + p.v0)) != cudaSuccess) return e;
         }
         if (!c.dx && !c.dw) continue;
         p.tn = L.tn_products;
+        const LossLaunch lp = loss_launch_of<PRODUCTS>(false, L.g_planes);
+        ring_of(p, lp.a_parts, lp.b_parts, c.dw ? BM : few, p.tn);
+        p.a_rows = few;
         const long long units = (c.dx ? (long long)L.s_dx * row_tiles * p.ht : 0) + (c.dw ? (long long)L.s_dw * cdiv(p.cols, BM) * p.ht : 0);
-        if ((e = launch_gemm(loss_launch_of<PRODUCTS>(false, L.g_planes), units, sms, map_g, map_w64, map_g64, map_x64, p, c.stream)) != cudaSuccess) return e;
+        if ((e = launch_gemm(lp, units, sms, map_g, map_w64, map_g64, map_x64, p, c.stream)) != cudaSuccess) return e;
         if (c.dw && L.slab_dw) {
             void* out = static_cast<uint8_t*>(c.dw) + (size_t)p.v0 * c.lddw * es;
-            if (f32) loss_sum_kernel<true><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdw, L.s_dw, L.piece, p.cols, c.o.H, L.Hp, nullptr, out, c.lddw, p.dw_vec);
-            else loss_sum_kernel<false><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdw, L.s_dw, L.piece, p.cols, c.o.H, L.Hp, nullptr, out, c.lddw, p.dw_vec);
-            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+            if ((e = launch_small(sum_kernel, sum_blocks, c.stream, ctrl, p.sdw, L.s_dw, L.piece, p.cols, c.o.H, L.Hp, nullptr, out, c.lddw, p.dw_vec)) !=
+                cudaSuccess)
+                return e;
         }
     }
-    if (c.dx && L.slab_dx) {
-        if (f32) loss_sum_kernel<true><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdx, L.s_dx, L.Npad, 0, c.o.H, L.Hp, r.src, c.dx, c.lddx, p.dx_vec);
-        else loss_sum_kernel<false><<<sum_blocks, 256, 0, c.stream>>>(ctrl, p.sdx, L.s_dx, L.Npad, 0, c.o.H, L.Hp, r.src, c.dx, c.lddx, p.dx_vec);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    }
+    if (c.dx && L.slab_dx)
+        return launch_small(sum_kernel, sum_blocks, c.stream, ctrl, p.sdx, L.s_dx, L.Npad, 0, c.o.H, L.Hp, r.src, c.dx, c.lddx, p.dx_vec);
     return cudaSuccess;
 }
 

@@ -177,12 +177,12 @@ def test_distill_loss_and_gradient(pkg, dtype, N, H, V, K):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("K", [0, 5])
+@pytest.mark.parametrize("N", [100, 300])
 @pytest.mark.parametrize("rows", ["none", "all", "last", "first", "every_other"])
-def test_padding(pkg, dtype, K, rows):
-    N = 300
+def test_padding(pkg, dtype, K, N, rows):
     c = make(3, dtype, N, 72, 140, K, pad=0.0, full=True)
     r = torch.arange(N, device=DEV)
-    out = {"none": r < 0, "all": r >= 0, "last": r >= 200, "first": r < 200, "every_other": r % 2 == 0}[rows]
+    out = {"none": r < 0, "all": r >= 0, "last": r >= 2 * N // 3, "first": r < 2 * N // 3, "every_other": r % 2 == 0}[rows]
     c["x"][out] = math.nan
     c["dloss"][out] = math.nan
     if K:
@@ -410,7 +410,7 @@ def test_arguments_are_checked(pkg):
     pkg.wind_label_loss(**ok, check=True)
     for k, bad in (("x", c["x"].float()), ("x", c["x"][:, :32]), ("x", c["x"].t().contiguous().t()), ("x", c["x"].cpu()), ("target", c["t"].long()),
                    ("target", c["t"][:5]), ("loss", v.double()), ("loss", v[:3]), ("lse", v.cpu()), ("bias", c["b"].bfloat16()), ("bias", c["b"][:7]),
-                   ("weight", c["w"].half()), ("weight", c["w"][0]), ("workspace", ws.cpu())):
+                   ("weight", c["w"].half()), ("weight", c["w"][0]), ("workspace", ws.cpu()), ("workspace", ws.int()), ("target", None), ("loss", None)):
         with pytest.raises(ValueError):
             pkg.wind_label_loss(**{**ok, k: bad})
     with pytest.raises(pkg.WindError) as e:
