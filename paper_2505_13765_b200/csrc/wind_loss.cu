@@ -721,15 +721,17 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = tmem_slot;
-    let_next_start();
     wait_for_previous();
     const int n_rows = p.ctrl->n_rows;
     const long long n_units = count_units<MODE>(p, n_rows);
+    // a short kernel lets the next one start at once; blocks that wait beside a long one slow it (two per cent of a text model's step)
+    if (n_units <= gridDim.x) let_next_start();
 
     if (warp == 0) {
         if (elect_one()) {
             int s = 0;
             uint32_t turn = 0;       // of the ring: stage s is used for the (turn + 1)-th time
+            uint8_t* a = smem;       // of stage s
             bool ok = true;
             for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 const Unit t = unit_of<MODE>(p, n_rows, u);
@@ -738,7 +740,6 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const uint32_t bytes = A_PARTS * a_part + B_PARTS * (MODE == PRODUCTS ? panels * PANEL_BYTES : p.tn * BK * 2);
                 for (int kb = t.k0; kb < t.k0 + t.nk; ++kb) {
                     if (!mbar_wait(&empty_bar[s], (turn & 1) ^ 1, &abort_flag)) { ok = false; break; }
-                    uint8_t* a = smem + (size_t)s * p.stage_bytes;
                     uint8_t* b = a + A_PARTS * a_part;
                     uint64_t* full = &full_bar[s];
                     mbar_expect_tx(full, bytes);
@@ -758,7 +759,8 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             for (int q = 0; q < panels; ++q)
                                 tma_load_3d(b + i * p.b_bytes + q * PANEL_BYTES, &map_b2, t.nt * p.tn + q * 64, kb * BK, i, full);
                     }
-                    if (++s == p.stages) { s = 0; ++turn; }
+                    a += p.stage_bytes;
+                    if (++s == p.stages) { s = 0; ++turn; a = smem; }
                 }
             }
             if (!ok) {   // given up: the copies in flight still write into this CTA's shared memory
@@ -772,7 +774,9 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     } else if (warp == 1) {
         if (elect_one()) {
             int s = 0;
-            uint32_t turn = 0, n_acc = 0;
+            uint32_t turn = 0, n_acc = 0, at = 0;                     // at: of stage s, in units of 16 bytes
+            const uint64_t major_k = smem_desc_sw128(smem_u32(smem)), major_mn = smem_desc_mn(smem_u32(smem));
+            const uint32_t stage = p.stage_bytes >> 4, b_bytes = p.b_bytes >> 4;
             bool ok = true;
             for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 const Unit t = unit_of<MODE>(p, n_rows, u);
@@ -781,7 +785,8 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const uint32_t idesc = idesc_bf16(BM, n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                 const uint64_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;   // 16 of K, in units of 16 bytes
                 uint32_t tm_d = 0;
-                const int a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2;
+                const uint32_t a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2 >> 4;
+                const uint64_t a0 = a_mn ? major_mn : major_k, b0 = (b_mn ? major_mn : major_k) + A_PARTS * a_part;
                 for (int i = 0; i < t.nk; ++i) {
                     const uint32_t acc = n_acc & 1u;
                     const bool first = KIND == F32 || i == 0, last = KIND == F32 || i == t.nk - 1;   // of an accumulator
@@ -791,17 +796,16 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     }
                     if (!mbar_wait(&full_bar[s], turn & 1, &abort_flag)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t a_addr = smem_u32(smem + (size_t)s * p.stage_bytes), b_addr = a_addr + A_PARTS * a_part;
-                    const uint64_t adesc = a_mn ? smem_desc_mn(a_addr) : smem_desc_sw128(a_addr);
-                    const uint64_t bdesc = b_mn ? smem_desc_mn(b_addr) : smem_desc_sw128(b_addr);
+                    const uint64_t adesc = a0 + at, bdesc = b0 + at;
 #pragma unroll
                     for (int term = 0; term < S::TERMS; ++term) {
-                        const uint64_t ad = adesc + S::a_part(term) * (a_part >> 4), bd = bdesc + S::b_part(term) * (p.b_bytes >> 4);
+                        const uint64_t ad = adesc + S::a_part(term) * a_part, bd = bdesc + S::b_part(term) * b_bytes;
 #pragma unroll
                         for (int k = 0; k < BK / 16; ++k) tc_mma_bf16(tm_d, ad + k * a_step, bd + k * b_step, idesc, !first || (term | k) != 0);
                     }
                     tc_commit(&empty_bar[s]);
-                    if (++s == p.stages) { s = 0; ++turn; }
+                    at += stage;
+                    if (++s == p.stages) { s = 0; ++turn; at = 0; }
                     if (last) { tc_commit(&acc_full[acc]); ++n_acc; }
                 }
             }
