@@ -62,6 +62,7 @@ struct RowsParams {
     int row_blocks;            // blocks of loss_gather that take rows; those behind them lay W out
     const void* w; int64_t ldw; int w_vec; __nv_bfloat16* wc;
     float* db;                 // where its only writers are the tiles of logits
+    const void* dw;
     int counted;               // counts[] holds the rows that count, of every ROWS_COUNTED rows
     int per_block;             // rows of a block of loss_gather, a multiple of 8
     float tau;
@@ -80,29 +81,35 @@ __device__ __forceinline__ uint8_t row_mark(const RowsParams& p, int r) {
     return t == -1 ? ROW_NONE : (t >= 0 && t < p.n_out ? ROW_COUNTS : ROW_BAD);
 }
 
+constexpr uint32_t NO_LABEL = 0xffffffu;   // (n_out is below 2^24)
+
 // The teacher's list of a row, a warp each: probabilities over the entries that are there, and the entries by rising label (equal
-// labels in their order), so that the epilogues walk a list along their columns.  The place of an entry is the number of entries
-// before it: K^2 / 32 comparisons a lane.
+// labels in their order), so that the epilogues walk a list along their columns.  The place of an entry is the number of keys
+// label * 256 + entry below its own: K^2 / 32 comparisons a lane.
 __global__ void __launch_bounds__(256) loss_list_kernel(const RowsParams p) {
-    __shared__ int32_t s_ids[8][kLossMaxK];
+    __shared__ __align__(16) uint32_t s_keys[8][kLossMaxK];
     let_next_start();
     wait_for_previous();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r = blockIdx.x * 8 + warp;
     if (r >= p.N) return;
-    int32_t* list = s_ids[warp];
+    uint32_t* keys = s_keys[warp];
     const int32_t* ids = p.ids + (size_t)r * p.K;
     const float* y = p.y + (size_t)r * p.K;
     float top = -CUDART_INF_F;
     int flags = 0;   // 1: an entry outside the outputs, 2: NaN
-    for (int k = lane; k < p.K; k += 32) {
-        const int id = ids[k];
-        const float v = y[k];
-        if (id < -1 || id >= p.n_out) flags |= 1;
-        const bool there = id >= 0 && id < p.n_out;
-        if (there && v != v) flags |= 2;
-        if (there) top = fmaxf(top, v);
-        list[k] = there ? id : 0x7fffffff;
+    for (int k = lane; k < (p.K + 3) / 4 * 4; k += 32) {
+        uint32_t key = 0xffffffffu;      // (behind the list: below no key)
+        if (k < p.K) {
+            const int id = ids[k];
+            const float v = y[k];
+            if (id < -1 || id >= p.n_out) flags |= 1;
+            const bool there = id >= 0 && id < p.n_out;
+            if (there && v != v) flags |= 2;
+            if (there) top = fmaxf(top, v);
+            key = (there ? (uint32_t)id : NO_LABEL) << 8 | (uint32_t)k;
+        }
+        keys[k] = key;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -112,23 +119,26 @@ __global__ void __launch_bounds__(256) loss_list_kernel(const RowsParams p) {
     __syncwarp();
     float sum = 0.f;
     for (int k = lane; k < p.K; k += 32)
-        if (list[k] != 0x7fffffff && y[k] != -CUDART_INF_F) sum += expf((y[k] - top) / p.tau);
+        if (keys[k] >> 8 != NO_LABEL && y[k] != -CUDART_INF_F) sum += expf((y[k] - top) / p.tau);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float log_sum = logf(sum);
     float ent = 0.f;
     for (int k = lane; k < p.K; k += 32) {
-        const int id = list[k];
+        const uint32_t key = keys[k];
         float q = 0.f;
-        if (id != 0x7fffffff && y[k] != -CUDART_INF_F) {
+        if (key >> 8 != NO_LABEL && y[k] != -CUDART_INF_F) {
             const float d = (y[k] - top) / p.tau;
             q = expf(d) / sum;
             if (q != 0.f) ent += q * (d - log_sum);
         }
         int place = 0;
 #pragma unroll 4
-        for (int j = 0; j < p.K; ++j) place += list[j] < id || (list[j] == id && j < k);
-        p.sid[(size_t)r * p.K + place] = id;
+        for (int j = 0; j < p.K; j += 4) {
+            const uint4 o = *reinterpret_cast<const uint4*>(keys + j);
+            place += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
+        }
+        p.sid[(size_t)r * p.K + place] = key >> 8 == NO_LABEL ? 0x7fffffff : (int)(key >> 8);
         p.sq[(size_t)r * p.K + place] = q;
     }
 #pragma unroll
@@ -279,11 +289,20 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
         }
         first *= ROWS_COUNTED;
     }
-#pragma unroll 8
-    for (int r = first + (int)threadIdx.x; r < r0; r += 256) {
-        const uint8_t m = row_mark(p, r);
-        before += m == ROW_COUNTS;
-        bad |= m == ROW_BAD;
+    for (int r = first + (int)threadIdx.x; r < r0; r += 8 * 256) {
+        if (p.K) {
+            uint8_t m[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[i] = r + i * 256 < r0 ? p.mark[r + i * 256] : (uint8_t)ROW_NONE;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { before += m[i] == ROW_COUNTS; bad |= m[i] == ROW_BAD; }
+        } else {
+            int t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = r + i * 256 < r0 ? p.target[r + i * 256] : -1;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { before += t[i] >= 0 && t[i] < p.n_out; bad |= t[i] < -1 || t[i] >= p.n_out; }
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
@@ -332,13 +351,15 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
         }
     }
     if ((int)blockIdx.x == p.row_blocks - 1) {
-        // the last row tile is full of zeros behind the last row
+        // dW sums over K blocks of 64 rows: zeros behind the last one.  (Other products only make rows of it that nobody looks at.)
         if (threadIdx.x == 0) {   // (this block has seen every mark)
             p.ctrl->status = bad ? WIND_ERR_INVALID_ARG : WIND_OK;
             p.ctrl->n_rows = total;
         }
         const float zero[8] = {};
-        for (int j = total + warp; j < (total + 127) / 128 * 128; j += 8)
+        if (p.dw)
+            for (int j = total + warp; j < (total + 63) / 64 * 64; j += 8)
+               
             for (int c = lane * 8; c < p.Hp; c += 256) store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, zero);
         if (p.db && total == 0)      // (no tile of logits is there to write it)
             for (int v = threadIdx.x; v < p.n_out; v += 256) p.db[v] = 0.f;
@@ -382,9 +403,9 @@ struct Shape {
     static constexpr int A_PARTS = KIND == F32 ? 3 : (KIND == BF16_FINE && MODE == PRODUCTS ? 2 : 1), B_PARTS = KIND == F32 ? 3 : 1;
     static constexpr int TERMS = KIND == F32 ? 6 : A_PARTS;
     static constexpr int WORST = A_PARTS * A_STAGE_BYTES + B_PARTS * TN * BK * 2;            // bytes of a full stage
-    // Groups of four epilogue warps (one per tensor-memory lane quadrant), each with its columns of a tile.  The gradient's share of
-    // logits takes more of the ALUs than the softmax's sums do: 16 warps hide more of it than 8.
-    static constexpr int GROUPS = MODE == LOGITS && KIND != F32 ? 4 : 2;
+    // Groups of four epilogue warps (one per tensor-memory lane quadrant), each with its columns of a tile.  A row of logits is a chain
+    // of maxima, exponentials and sums: 16 warps hide more of it than 8 (which is what fp32's sums leave registers for).
+    static constexpr int GROUPS = MODE != PRODUCTS && KIND != F32 ? 4 : 2;
     static constexpr int EPI = 128 * GROUPS, THREADS = 64 + EPI, CHUNKS = TN / GROUPS / 32;
     // Part products, smallest first: the parts of A and B of each (fp32: 20 02 11 10 01 00; fine: 10 00).
     static __device__ __forceinline__ constexpr int a_part(int t) { return KIND == F32 ? (0x001102 >> (4 * t)) & 3 : TERMS - 1 - t; }
@@ -536,41 +557,50 @@ struct Targets {
     }
 };
 
+// What a row's softmax has of some columns: their maximum, the sum of exponentials against it, the targets' weighted logits.
+struct RowPart { float m, s, qz; };
+__device__ __forceinline__ void join(RowPart& a, float m, float s, float qz) {
+    const float m1 = fmaxf(a.m, m), base = m1 == -CUDART_INF_F ? 0.f : m1;
+    a.s = a.s * exp2_fast((a.m - base) * kLog2e) + s * exp2_fast((m - base) * kLog2e);
+    a.m = m1;
+    a.qz += qz;
+}
+
 // FORWARD epilogue of one row's columns (n_cols of them are outputs) from `col` on.
 template <bool LIST, int KIND, int CHUNKS>
-__device__ __forceinline__ void forward_row(const LossGemm& p, uint32_t taddr, const float* sums, const float* bias, int col, int n_cols, int row,
-                                            int n_rows, int part) {
-    float m = -CUDART_INF_F, s = 0.f, qz = 0.f;
-    Targets<LIST> targets(p, row, row < n_rows, col);
+__device__ __forceinline__ RowPart forward_row(const LossGemm& p, uint32_t taddr, const float* sums, const float* bias, int col, int n_cols,
+                                               Targets<LIST>& targets) {
+    RowPart part{-CUDART_INF_F, 0.f, 0.f};
     constexpr int UNROLL = KIND == F32 ? CHUNKS : 1;
 #pragma unroll UNROLL
     for (int c = 0; c < CHUNKS; ++c) {
         if (c * 32 >= n_cols) continue;
         float v[32];
         fetch32<KIND>(v, taddr, sums, c);
-        float top = -CUDART_INF_F;
+        float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+        const float4* b4 = reinterpret_cast<const float4*>(bias + c * 32);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            v[i] = (v[i] + bias[c * 32 + i]) * p.rtau;
-            top = fmaxf(top, v[i]);
+        for (int i = 0; i < 32; i += 4) {
+            const float4 b = b4[i / 4];
+            v[i] = (v[i] + b.x) * p.rtau; v[i + 1] = (v[i + 1] + b.y) * p.rtau; v[i + 2] = (v[i + 2] + b.z) * p.rtau; v[i + 3] = (v[i + 3] + b.w) * p.rtau;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], v[i + k]);
         }
+        float qz = 0.f;
         targets.in(col + c * 32, [&](int at, float q) {
             const float z = pick32(v, at);
             if (q != 0.f) qz += q * z;
         });
-        const float m1 = fmaxf(m, top), base = m1 == -CUDART_INF_F ? 0.f : m1;
-        float add = 0.f;
+        const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const float m1 = fmaxf(part.m, m), base = m1 == -CUDART_INF_F ? 0.f : m1;
+        float add[4] = {};
 #pragma unroll
-        for (int i = 0; i < 32; ++i) add += exp2_fast((v[i] - base) * kLog2e);
-        s = s * exp2_fast((m - base) * kLog2e) + add;
-        m = m1;
+        for (int i = 0; i < 32; ++i) add[i & 3] += exp2_fast((v[i] - base) * kLog2e);
+        part.s = part.s * exp2_fast((part.m - base) * kLog2e) + ((add[0] + add[1]) + (add[2] + add[3]));
+        part.m = m1;
+        part.qz += qz;
     }
-    if (row < n_rows) {
-        const size_t at = (size_t)part * p.Npad + row;
-        p.pm[at] = m;
-        p.ps[at] = s;
-        p.pq[at] = qz;
-    }
+    return part;
 }
 
 // Sums over the 32 lanes of 32 values each: lane l gets the sum of value l.
@@ -591,11 +621,8 @@ __device__ __forceinline__ float column_sums(float* v, int lane) {
 // the columns' sums.
 template <bool LIST, int KIND, int CHUNKS>
 __device__ __forceinline__ void logits_row(const LossGemm& p, uint32_t taddr, const float* sums, const float* bias, int g_col, int n_cols, int row,
-                                           int n_rows, float* col_sums) {
+                                           bool there, float scale, float nlse, Targets<LIST>& targets, float* col_sums) {
     const int lane = threadIdx.x & 31, col = p.v0 + g_col;
-    const bool there = row < n_rows;
-    const float scale = there ? p.scale[row] : 0.f, nlse = there ? p.nlse[row] : 0.f;
-    Targets<LIST> targets(p, row, there, col);
     __nv_bfloat16* dst = p.g + (size_t)row * p.ldg + g_col;
     const int g_end = (p.cols + 63) / 64 * 64 - g_col;
     constexpr int UNROLL = KIND == F32 ? CHUNKS : 1;
@@ -607,7 +634,12 @@ __device__ __forceinline__ void logits_row(const LossGemm& p, uint32_t taddr, co
         if (some) {
             fetch32<KIND>(v, taddr, sums, c);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = scale * exp2_fast(((v[i] + bias[c * 32 + i]) * p.rtau - nlse) * kLog2e);
+            for (int i = 0; i < 32; i += 4) {
+                const float4 b = reinterpret_cast<const float4*>(bias + c * 32)[i / 4];
+                const float bb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[i + k] = scale * exp2_fast(((v[i + k] + bb[k]) * p.rtau - nlse) * kLog2e);
+            }
             targets.in(col + c * 32, [&](int at, float q) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = at == i ? v[i] - scale * q : v[i];
@@ -701,8 +733,9 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     __shared__ uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], acc_full[2], acc_empty[2], drain_bar;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
-    __shared__ float s_bias[2][TN];
-    __shared__ float s_db[4][TN];     // [lane quadrant][column of the tile]
+    __shared__ __align__(16) float s_bias[2][TN];
+    __shared__ float s_part[MODE == FORWARD ? S::GROUPS : 1][3][BM];   // [group][maximum, sum, targets' logits][row]
+    __shared__ float s_db[MODE == LOGITS ? 4 : 1][TN];     // [lane quadrant][column of the tile]
 
     const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
     uint8_t* smem = align_smem_1024(smem_raw);
@@ -828,6 +861,11 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint32_t lanes = tmem_base + my0 + ((uint32_t)(q * 32) << 16);
             const int row = t.mt * BM + row_in_tile;
             float* bias = s_bias[n_tile & 1];
+            // what the row needs besides its logits, under way while these are made
+            const bool there = row < n_rows;
+            const int col = p.v0 + t.nt * p.tn + my0;
+            Targets<LIST> targets(p, row, MODE != PRODUCTS && there && my0 < p.tn, col);
+            const float scale = MODE == LOGITS && there ? p.scale[row] : 0.f, nlse = MODE == LOGITS && there ? p.nlse[row] : 0.f;
             if (MODE != PRODUCTS) {
                 if (et < p.tn) {
                     const int v = p.v0 + t.nt * p.tn + et;     // outputs behind the last one: probability zero
@@ -867,12 +905,12 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 tc_fence_after();
                 taddr = lanes + acc * TN;
             }
+            RowPart part{-CUDART_INF_F, 0.f, 0.f};
             if (ok && my0 < p.tn) {
                 if constexpr (MODE == FORWARD) {
-                    const int col = t.nt * p.tn + my0, n_cols = min(width, p.n_out - col);
-                    if (n_cols > 0) forward_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, col, n_cols, row, n_rows, col / width);
+                    part = forward_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, col, min(width, p.n_out - col), targets);
                 } else if constexpr (MODE == LOGITS) {
-                    logits_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, t.nt * p.tn + my0, width, row, n_rows, &s_db[q][my0]);
+                    logits_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, t.nt * p.tn + my0, width, row, there, scale, nlse, targets, &s_db[q][my0]);
                 } else {
                     product_row<KIND, S::CHUNKS>(p, t, taddr, sums, t.nt * p.tn + my0, row_in_tile, n_rows, t.nk == 0);
                 }
@@ -882,6 +920,20 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&acc_empty[n_acc & 1u]);
                 ++n_acc;
+            }
+            if constexpr (MODE == FORWARD) {
+                // the groups' parts of a row become one
+                if (group) { s_part[group][0][row_in_tile] = part.m; s_part[group][1][row_in_tile] = part.s; s_part[group][2][row_in_tile] = part.qz; }
+                __syncwarp();
+                asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
+                if (group == 0 && there) {
+#pragma unroll
+                    for (int i = 1; i < S::GROUPS; ++i) join(part, s_part[i][0][row_in_tile], s_part[i][1][row_in_tile], s_part[i][2][row_in_tile]);
+                    const size_t at = (size_t)t.nt * p.Npad + row;
+                    p.pm[at] = part.m;
+                    p.ps[at] = part.s;
+                    p.pq[at] = part.qz;
+                }
             }
             if (MODE == LOGITS && p.dbp) {
                 __syncwarp();
@@ -1041,7 +1093,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad) {
     L.w = take(L.pack_w ? 2 * (size_t)L.planes * o.n_out * L.Hp : 0);
     if (!grad) {
         L.tn = tile_cols(L.Npad / BM, o.n_out, most);
-        L.parts = cdiv(o.n_out, group_cols(L.tn, f32 ? Shape<FORWARD, F32>::GROUPS : Shape<FORWARD, BF16>::GROUPS));
+        L.parts = cdiv(o.n_out, L.tn);
         const size_t parts = (size_t)L.parts;
         L.pm = take(4 * parts * np);
         L.ps = take(4 * parts * np);
@@ -1225,6 +1277,7 @@ cudaError_t loss_run(const LossCall& c) {
     }
     const bool one_tile = L.Npad == BM;      // of rows: then the tiles of logits write db themselves
     if (c.grad && one_tile) r.db = c.db;
+    if (c.grad) r.dw = c.dw;
     if ((e = launch_small(f32 ? loss_gather_kernel<true> : loss_gather_kernel<false>, r.row_blocks + pack_blocks, c.stream, r)) != cudaSuccess) return e;
 
     LossGemm p{};

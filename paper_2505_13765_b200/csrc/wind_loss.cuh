@@ -10,7 +10,7 @@ namespace wind {
 
 constexpr int kLossMaxK = 256;            // teacher's entries of a row
 constexpr int kLossMaxRows = 1 << 24;
-constexpr int kLossMaxOut = 1 << 24;
+constexpr int kLossMaxOut = (1 << 24) - 1;
 constexpr int kLossMaxH = 1 << 16;
 constexpr size_t kLossPieceBytes = (size_t)512 << 20;   // the gradient's share of logits that is kept at a time (see loss_layout)
 
