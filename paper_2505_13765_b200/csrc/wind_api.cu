@@ -487,7 +487,7 @@ wind_status_t wind_loss_workspace_bytes(const wind_output_t* o, int32_t N, int32
     wind_status_t s = check_output(o, N, K);
     if (s != WIND_OK) return s;
     if (!bytes) return WIND_ERR_INVALID_ARG;
-    *bytes = loss_layout(*o, N, K, grad != 0).total;
+    *bytes = loss_layout(*o, N, K, grad != 0, true).total;
     return WIND_OK;
 }
 

@@ -16,7 +16,7 @@
 //                   PRODUCTS  dx += g W and dW = g^T x of that piece, g as both operands' layouts need it: rows are contiguous along
 //                             the outputs, which is K of the first product and M of the second (the matrix descriptors take either)
 //     loss_combine  a row's partial results to its loss and log-sum-exp
-//     loss_sum      partial sums of dx / dW, where a product is cut along its K to fill the chip; loss_bias: db
+//     loss_finish   partial sums of dx / dW, where a product is cut along its K to fill the chip; db
 //
 // fp32 operands are cut into three bf16 parts, x = x1 + x2 + x3 with 8 bits each, and a product into the six of nine part products
 // that are not below 2^-24 of it: x1 w1 + (x1 w2 + x2 w1) + (x1 w3 + x2 w2 + x3 w1), smallest first, in one fp32 accumulator.
@@ -44,9 +44,10 @@ namespace wind {
 // sizes
 // ---------------------------------------------------------------------------
 constexpr int LT_BAND = 16;               // row tiles that are worked on together (see tile_of)
-constexpr int ROWS_COUNTED = 8192;        // longer calls have the rows that count counted by a kernel of its own, so many at a time
+constexpr int ROWS_COUNTED = 32768;       // longer calls have the rows that count counted by a kernel of its own, so many at a time
 constexpr int PANEL_BYTES = 64 * BK * 2;  // 64 x 64 bf16
 constexpr int kFillCtas = 148;            // CTAs that a product is cut for
+constexpr int kNarrowTiles = 4 * kFillCtas;   // so many tiles or more are not made narrower, nor their sums cut
 
 static inline int up(long long a, int b) { return (int)((a + b - 1) / b * b); }
 static inline int cdiv(long long a, int b) { return (int)((a + b - 1) / b); }
@@ -59,6 +60,7 @@ enum Mark : uint8_t { ROW_NONE = 0, ROW_COUNTS = 1, ROW_BAD = 2 };   // BAD: a l
 struct RowsParams {
     LossCtrl* ctrl;
     int N, n_out, K, H, Hp, Npad, x_vec, grad;
+    int32_t* next; int n_next; // units taken by the products' kernels
     int row_blocks;            // blocks of loss_gather that take rows; those behind them lay W out
     const void* w; int64_t ldw; int w_vec; __nv_bfloat16* wc;
     float* db;                 // where its only writers are the tiles of logits
@@ -289,19 +291,40 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
         }
         first *= ROWS_COUNTED;
     }
-    for (int r = first + (int)threadIdx.x; r < r0; r += 8 * 256) {
-        if (p.K) {
-            uint8_t m[8];
+    // (first and r0 are multiples of 8)
+    if (p.K) {
+        for (int r = first + 8 * (int)threadIdx.x; r < r0; r += 8 * 4 * 256) {
+            uint2 m[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m[i] = r + i * 256 < r0 ? p.mark[r + i * 256] : (uint8_t)ROW_NONE;
+            for (int i = 0; i < 4; ++i) m[i] = r + i * 2048 < r0 ? *reinterpret_cast<const uint2*>(p.mark + r + i * 2048) : make_uint2(0, 0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { before += m[i] == ROW_COUNTS; bad |= m[i] == ROW_BAD; }
-        } else {
-            int t[8];
+            for (int i = 0; i < 4; ++i) {
+                before += __popc(m[i].x & 0x01010101u) + __popc(m[i].y & 0x01010101u);
+                bad |= ((m[i].x | m[i].y) & 0x02020202u) != 0;
+            }
+        }
+    } else {
+        const bool vec = reinterpret_cast<uintptr_t>(p.target) % 16 == 0;
+        for (int r = first + 4 * (int)threadIdx.x; r < r0; r += 4 * 8 * 256) {
+            int t[8][4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = r + i * 256 < r0 ? p.target[r + i * 256] : -1;
+            for (int i = 0; i < 8; ++i) {
+                const int at = r + i * 1024;
+                if (at >= r0) { t[i][0] = t[i][1] = t[i][2] = t[i][3] = -1; }
+                else if (vec) {
+                    const int4 q = *reinterpret_cast<const int4*>(p.target + at);
+                    t[i][0] = q.x; t[i][1] = q.y; t[i][2] = q.z; t[i][3] = q.w;
+                } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { before += t[i] >= 0 && t[i] < p.n_out; bad |= t[i] < -1 || t[i] >= p.n_out; }
+                    for (int k = 0; k < 4; ++k) t[i][k] = p.target[at + k];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int v = t[i / 4][i % 4];
+                before += v >= 0 && v < p.n_out;
+                bad |= v < -1 || v >= p.n_out;
+            }
         }
     }
 #pragma unroll
@@ -356,6 +379,7 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
             p.ctrl->status = bad ? WIND_ERR_INVALID_ARG : WIND_OK;
             p.ctrl->n_rows = total;
         }
+        for (int i = threadIdx.x; i < p.n_next; i += 256) p.next[i] = 0;
         const float zero[8] = {};
         if (p.dw)
             for (int j = total + warp; j < (total + 63) / 64 * 64; j += 8)
@@ -382,6 +406,7 @@ struct LossGemm {
     int a_rows;                   // rows that a fetch of x, or of g for dx, brings; b_bytes: what lies between the parts of B
     int b_bytes;
     int v0, cols, n_vt;           // this piece's first output, its outputs (to n_out at most) and tiles
+    int32_t* next;                // units that were taken, beyond the CTAs' first ones
     float rtau;                   // 1 / tau
     const float* bias;
     const int32_t* src; const int32_t* target; const int32_t* sid; const float* sq;
@@ -389,6 +414,7 @@ struct LossGemm {
     const float* scale; const float* nlse;
     __nv_bfloat16* g; int ldg; size_t g_plane; float* dbp;   // LOGITS
     // PRODUCTS
+    int dx_first;                 // whether dx's units are the longer ones
     int ht, s_dx, s_dw, add_dx;   // tiles of H, parts of the sums, whether dx's partial sums are added to
     float *sdx, *sdw; int slab_rows_dw;   // partial sums, or null: straight to dx / dw
     void* dx; int64_t lddx; int dx_vec; int want_dx;         // vec: what rows are aligned to, 0: nothing, 1: 16 bytes, 2: 32 bytes
@@ -478,23 +504,32 @@ __device__ __forceinline__ long long count_units(const LossGemm& p, int n_rows) 
     return n;
 }
 
-// Logits: bands of LT_BAND row tiles, in a band row tile fastest, so that the CTAs at work share few tiles of x and of W.
+// Logits: bands of LT_BAND row tiles, in a band row tile fastest, so that the CTAs at work share few tiles of x and of W; last tiles of
+// at most half the columns (1024 labels and the blank) come behind all others.  Products: the longer ones first.  CTAs take the next
+// unit when they are through with one, and what is short at the end fills the gaps.
 template <int MODE>
 __device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long u) {
     Unit t{};
     const int mtc = (n_rows + BM - 1) / BM;
     if (MODE != PRODUCTS) {
-        const long long per_band = (long long)LT_BAND * p.n_vt;
-        const int band = (int)(u / per_band);
+        const int rest = p.cols - (p.n_vt - 1) * p.tn, wide = p.n_vt - (p.n_vt > 1 && 2 * rest <= p.tn);
+        t.nk = p.kb;
+        const long long n_wide = (long long)mtc * wide;
+        if (u >= n_wide) {
+            t.nt = wide;
+            t.mt = (int)(u - n_wide);
+            return t;
+        }
+        const long long per_band = (long long)LT_BAND * wide;
+        const int band = u < 0x7fffffff && per_band < 0x7fffffff ? (int)((uint32_t)u / (uint32_t)per_band) : (int)(u / per_band);
         const int r = (int)(u - band * per_band), in_band = min(LT_BAND, mtc - band * LT_BAND);
         t.nt = r / in_band;
         t.mt = band * LT_BAND + (r - t.nt * in_band);
-        t.nk = p.kb;
         return t;
     }
-    const long long n_dx = p.want_dx ? (long long)p.s_dx * mtc * p.ht : 0;
-    t.dw = u >= n_dx;
-    if (t.dw) u -= n_dx;
+    const long long n_dx = p.want_dx ? (long long)p.s_dx * mtc * p.ht : 0, n_dw = p.want_dw ? (long long)p.s_dw * ((p.cols + BM - 1) / BM) * p.ht : 0;
+    t.dw = p.dx_first ? u >= n_dx : u < n_dw;
+    if (t.dw == p.dx_first) u -= t.dw ? n_dx : n_dw;
     const int tiles = (t.dw ? (p.cols + BM - 1) / BM : mtc) * p.ht;
     t.part = (int)(u / tiles);
     const int r = (int)(u - (long long)t.part * tiles);
@@ -504,6 +539,22 @@ __device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long
     t.k0 = (int)((long long)kb * t.part / s);
     t.nk = (int)((long long)kb * (t.part + 1) / s) - t.k0;
     return t;
+}
+
+// A CTA's first unit is that of its number; the others are handed on through a ring, by the one thread that fetches operands and
+// takes them, to the one that issues the products and to the epilogue.
+constexpr int UNITS = 4;
+struct UnitRing {
+    uint64_t full[UNITS], empty[UNITS];
+    long long unit[UNITS];
+};
+// The n-th unit behind the first, or -1: none is left, or the wait ran out.
+__device__ __forceinline__ long long next_unit(UnitRing& ring, uint32_t n, volatile int* abort_flag) {
+    const uint32_t i = n % UNITS;
+    if (!mbar_wait(&ring.full[i], (n / UNITS) & 1, abort_flag)) return -1;
+    const long long u = *reinterpret_cast<volatile long long*>(&ring.unit[i]);
+    mbar_arrive(&ring.empty[i]);
+    return u;
 }
 
 template <int MODE>
@@ -731,8 +782,10 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     constexpr int TN = S::TN, EPI = S::EPI, A_PARTS = S::A_PARTS, B_PARTS = S::B_PARTS;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], acc_full[2], acc_empty[2], drain_bar;
+    __shared__ UnitRing units;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
+    __shared__ long long s_unit[2];
     __shared__ __align__(16) float s_bias[2][TN];
     __shared__ float s_part[MODE == FORWARD ? S::GROUPS : 1][3][BM];   // [group][maximum, sum, targets' logits][row]
     __shared__ float s_db[MODE == LOGITS ? 4 : 1][TN];     // [lane quadrant][column of the tile]
@@ -744,6 +797,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         abort_flag = 0;
         for (int s = 0; s < p.stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], EPI / 32); }
+        for (int i = 0; i < UNITS; ++i) { mbar_init(&units.full[i], 1); mbar_init(&units.empty[i], 2); }
         mbar_init(&drain_bar, 1);
         fence_barrier_init();
         prefetch_tmap(&map_a); prefetch_tmap(&map_b);
@@ -760,17 +814,32 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // a short kernel lets the next one start at once; blocks that wait beside a long one slow it (two per cent of a text model's step)
     if (n_units <= gridDim.x) let_next_start();
 
+    const long long first = blockIdx.x < n_units ? (long long)blockIdx.x : -1;
+
     if (warp == 0) {
         if (elect_one()) {
             int s = 0;
             uint32_t turn = 0;       // of the ring: stage s is used for the (turn + 1)-th time
             uint8_t* a = smem;       // of stage s
             bool ok = true;
-            for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+            long long u = first;
+            for (uint32_t n = 0; u >= 0; ++n) {
+                const int taken = atomicAdd(p.next, 1);                     // (there when this unit's first K blocks are under way)
+                // The next unit is handed on once the ring is full of this one: at that point nothing waits for this unit's epilogue, which
+                // waits for the answer (and empties fp32's accumulators, without which the rest could not be fetched).
+                auto hand_on = [&] {
+                    if (!mbar_wait(&units.empty[n % UNITS], ((n / UNITS) & 1) ^ 1, &abort_flag)) return false;
+                    u = (long long)gridDim.x + taken;
+                    if (u >= n_units) u = -1;
+                    *reinterpret_cast<volatile long long*>(&units.unit[n % UNITS]) = u;
+                    mbar_arrive(&units.full[n % UNITS]);
+                    return true;
+                };
                 const Unit t = unit_of<MODE>(p, n_rows, u);
                 const int panels = (unit_cols<MODE>(p, t) + 63) / 64;
                 const int a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2;
                 const uint32_t bytes = A_PARTS * a_part + B_PARTS * (MODE == PRODUCTS ? panels * PANEL_BYTES : p.tn * BK * 2);
+                const int hand_at = t.k0 + min(t.nk, p.stages) - 1;
                 for (int kb = t.k0; kb < t.k0 + t.nk; ++kb) {
                     if (!mbar_wait(&empty_bar[s], (turn & 1) ^ 1, &abort_flag)) { ok = false; break; }
                     uint8_t* b = a + A_PARTS * a_part;
@@ -794,7 +863,10 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     }
                     a += p.stage_bytes;
                     if (++s == p.stages) { s = 0; ++turn; a = smem; }
+                    if (kb == hand_at && !hand_on()) { ok = false; break; }
                 }
+                if (ok && t.nk == 0) ok = hand_on();
+                if (!ok) break;
             }
             if (!ok) {   // given up: the copies in flight still write into this CTA's shared memory
                 int late = 0;
@@ -811,7 +883,8 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint64_t major_k = smem_desc_sw128(smem_u32(smem)), major_mn = smem_desc_mn(smem_u32(smem));
             const uint32_t stage = p.stage_bytes >> 4, b_bytes = p.b_bytes >> 4;
             bool ok = true;
-            for (long long u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+            uint32_t n_unit = 0;
+            for (long long u = first; u >= 0 && ok; u = next_unit(units, n_unit++, &abort_flag)) {
                 const Unit t = unit_of<MODE>(p, n_rows, u);
                 const int n = (unit_cols<MODE>(p, t) + 31) / 32 * 32;   // (the epilogues read 32 columns at a time)
                 const bool a_mn = MODE == PRODUCTS && t.dw, b_mn = MODE == PRODUCTS;
@@ -842,7 +915,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     if (last) { tc_commit(&acc_full[acc]); ++n_acc; }
                 }
             }
-            if (!ok) {   // given up: the products in flight still read it
+            if (!ok || *reinterpret_cast<volatile int*>(&abort_flag)) {   // given up: the products in flight still read it
                 int late = 0;
                 tc_commit(&drain_bar);
                 mbar_wait(&drain_bar, 0, &late);
@@ -856,7 +929,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const int my0 = group * width;                     // first column of this warp's, in the tile
         uint32_t n_acc = 0, n_tile = 0;
         bool ok = true;
-        for (long long u = blockIdx.x; u < n_units; u += gridDim.x, ++n_tile) {
+        for (long long u = first; u >= 0; ++n_tile) {
             const Unit t = unit_of<MODE>(p, n_rows, u);
             const uint32_t lanes = tmem_base + my0 + ((uint32_t)(q * 32) << 16);
             const int row = t.mt * BM + row_in_tile;
@@ -866,15 +939,16 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const int col = p.v0 + t.nt * p.tn + my0;
             Targets<LIST> targets(p, row, MODE != PRODUCTS && there && my0 < p.tn, col);
             const float scale = MODE == LOGITS && there ? p.scale[row] : 0.f, nlse = MODE == LOGITS && there ? p.nlse[row] : 0.f;
-            if (MODE != PRODUCTS) {
-                if (et < p.tn) {
-                    const int v = p.v0 + t.nt * p.tn + et;     // outputs behind the last one: probability zero
-                    bias[et] = v < p.n_out ? (p.bias ? p.bias[v] : 0.f) : -CUDART_INF_F;
-                }
-                __syncwarp();
-                asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
+            if (MODE != PRODUCTS && et < p.tn) {
+                const int v = p.v0 + t.nt * p.tn + et;         // outputs behind the last one: probability zero
+                bias[et] = v < p.n_out ? (p.bias ? p.bias[v] : 0.f) : -CUDART_INF_F;
             }
-            // (a warp that gives up goes on without waiting: the others still meet it at the barriers)
+            // One thread asks for the next unit, which is there before this one's accumulator is; all warps hear the same answer, so that
+            // they leave together.  (A warp whose wait runs out goes on without waiting: the others still meet it at the barriers.)
+            if (et == 0) s_unit[n_tile & 1] = next_unit(units, n_tile, &abort_flag);
+            __syncwarp();
+            asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
+            u = s_unit[n_tile & 1];
             // fp32: an accumulator takes one K block, whose sum is added up here.  (Tensor cores cut where they add; over a long K that
             // is an error of 2^-25 an addition, all one way: 5e-6 of dW over 20 000 rows.)
             float sums[KIND == F32 ? S::CHUNKS * 32 : 1];
@@ -1004,20 +1078,26 @@ __global__ void __launch_bounds__(256) loss_combine_kernel(const LossCtrl* ctrl,
     lse[r] = m + log_s;
 }
 
-// Partial sums of dx (rows: those that count, to their places) or dW (rows: a piece's outputs).
+// What is left of a piece: partial sums of dW and, behind the last piece, of dx to their places, and db from the row tiles' column sums.
+struct FinishParams {
+    const LossCtrl* ctrl;
+    int H, Hp, blocks_dw, blocks_dx;      // blocks of either; those behind them are db's
+    const float* sdw; int s_dw, slab_rows_dw, cols; void* dw; int64_t lddw; int dw_vec;     // dw: of the piece's first output
+    const float* sdx; int s_dx, slab_rows_dx; const int32_t* src; void* dx; int64_t lddx; int dx_vec;
+    const float* dbp; int ld_dbp; float* db;
+};
+
 template <bool F32>
-__global__ void __launch_bounds__(256) loss_sum_kernel(const LossCtrl* ctrl, const float* slab, int parts, int slab_rows, int rows, int H, int Hp,
-                                                       const int32_t* src, void* out, int64_t ld, int vec) {
-    let_next_start();
-    wait_for_previous();
-    if (src) rows = ctrl->n_rows;
+__device__ __forceinline__ void sum_parts(const float* slab, int parts, int slab_rows, int rows, int H, int Hp, const int32_t* src, void* out, int64_t ld,
+                                          int vec, int block, int blocks) {
     const int per_row = (H + 3) / 4;
     const long long all = (long long)rows * per_row;
     const size_t stride = (size_t)slab_rows * Hp;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+    for (long long i = (long long)block * 256 + threadIdx.x; i < all; i += (long long)blocks * 256) {
         const int r = (int)(i / per_row), h = (int)(i - (long long)r * per_row) * 4;
         const float* at = slab + (size_t)r * Hp + h;
         float4 a = *reinterpret_cast<const float4*>(at);
+#pragma unroll 4
         for (int k = 1; k < parts; ++k) {
             const float4 b = *reinterpret_cast<const float4*>(at + k * stride);
             a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
@@ -1035,21 +1115,34 @@ __global__ void __launch_bounds__(256) loss_sum_kernel(const LossCtrl* ctrl, con
     }
 }
 
-// db of a piece: sums of the row tiles' column sums, 32 outputs x 8 slices a block.
-__global__ void __launch_bounds__(256) loss_bias_kernel(const LossCtrl* ctrl, const float* dbp, int ld, int cols, float* db) {
+template <bool F32>
+__global__ void __launch_bounds__(256) loss_finish_kernel(const FinishParams p) {
     __shared__ float s_sum[8][32];
     let_next_start();
     wait_for_previous();
-    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    const int tiles = (ctrl->n_rows + BM - 1) / BM;
+    const int n_rows = p.ctrl->n_rows;
+    int block = blockIdx.x;
+    if (block < p.blocks_dw) {
+        sum_parts<F32>(p.sdw, p.s_dw, p.slab_rows_dw, p.cols, p.H, p.Hp, nullptr, p.dw, p.lddw, p.dw_vec, block, p.blocks_dw);
+        return;
+    }
+    block -= p.blocks_dw;
+    if (block < p.blocks_dx) {
+        sum_parts<F32>(p.sdx, p.s_dx, p.slab_rows_dx, n_rows, p.H, p.Hp, p.src, p.dx, p.lddx, p.dx_vec, block, p.blocks_dx);
+        return;
+    }
+    block -= p.blocks_dx;
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, c = block * 32 + lane;     // 32 outputs x 8 slices
+    const int tiles = (n_rows + BM - 1) / BM;
     float sum = 0.f;
-    if (c < cols)
-        for (int i = slice; i < tiles; i += 8) sum += dbp[(size_t)i * ld + c];
+    if (c < p.cols)
+#pragma unroll 4
+        for (int i = slice; i < tiles; i += 8) sum += p.dbp[(size_t)i * p.ld_dbp + c];
     s_sum[slice][lane] = sum;
     __syncthreads();
-    if (slice || c >= cols) return;
+    if (slice || c >= p.cols) return;
     for (int i = 1; i < 8; ++i) sum += s_sum[i][lane];
-    db[c] = sum;
+    p.db[c] = sum;
 }
 
 // ---------------------------------------------------------------------------
@@ -1060,6 +1153,7 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const LossCtrl* ctrl, co
 static int tile_cols(int row_tiles, int cols, int most) {
     int best = most;
     long long least = 0;
+    if ((long long)row_tiles * cdiv(cols, most) >= kNarrowTiles) return most;
     for (int tn = most; tn >= 64; tn /= 2) {
         const long long time = (((long long)row_tiles * cdiv(cols, tn) + kFillCtas - 1) / kFillCtas) * (tn + 64);
         if (tn == most || time < least) { best = tn; least = time; }
@@ -1067,7 +1161,7 @@ static int tile_cols(int row_tiles, int cols, int most) {
     return best;
 }
 
-LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad) {
+LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most_of_fewer) {
     LossLayout L{};
     const bool f32 = o.dtype == WIND_DT_F32;
     L.planes = f32 ? 3 : 1;
@@ -1094,10 +1188,12 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad) {
     if (!grad) {
         L.tn = tile_cols(L.Npad / BM, o.n_out, most);
         L.parts = cdiv(o.n_out, L.tn);
-        const size_t parts = (size_t)L.parts;
-        L.pm = take(4 * parts * np);
-        L.ps = take(4 * parts * np);
-        L.pq = take(4 * parts * np);
+        L.next = take(4);
+        size_t parts = (size_t)L.parts * np;
+        if (most_of_fewer) parts = std::max((size_t)cdiv(o.n_out, most) * np, std::min((size_t)cdiv(o.n_out, 64) * np, (size_t)kNarrowTiles * (most / 64) * 128));
+        L.pm = take(4 * parts);
+        L.ps = take(4 * parts);
+        L.pq = take(4 * parts);
     } else {
         // a piece: as many outputs as keep its g within kLossPieceBytes, 2048 at least (below that the partial sums of dx, read and
         // written once a piece, cost more than a few per cent of the products)
@@ -1110,18 +1206,37 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad) {
         const int ht = cdiv(o.H, L.tn_products), terms = f32 ? 6 : 1;
         const long long t_dx = (long long)(L.Npad / 128) * ht, t_dw = (long long)cdiv(std::min(o.n_out, L.piece), 128) * ht;
         const int kb_dx = cdiv(std::min(o.n_out, L.piece), BK), kb_dw = L.Npad / BK;
+        // Parts of a sum: units of at most two thirds of a CTA's share of all K blocks, so that the units taken last fill the gaps, but of
+        // 8 K blocks (bf16) at least, and none where the tiles alone are many.
+        const int least_kb = cdiv(8, terms);
+        const long long work = t_dx * kb_dx + t_dw * kb_dw, share = (2 * work + 3 * kFillCtas - 1) / (3 * kFillCtas);
         auto parts_of = [&](long long tiles, int kb) {
-            if (tiles <= 0 || tiles >= kFillCtas) return 1;
-            return (int)std::max(1LL, std::min<long long>({kFillCtas / tiles, (long long)kb * terms / 8, (long long)kb}));
+            return tiles >= kNarrowTiles ? 1 : std::max(1, cdiv(kb, (int)std::min<long long>(std::max<long long>(share, least_kb), std::max(1, kb))));
         };
         L.s_dx = parts_of(t_dx, kb_dx);
         L.s_dw = parts_of(t_dw, kb_dw);
         L.slab_dx = L.s_dx > 1 || L.pieces > 1;
         L.slab_dw = L.s_dw > 1;
-        L.g = take(2 * (size_t)L.g_planes * np * L.piece);
-        L.dbp = take(4 * (np / 128) * L.piece);
-        L.sdx = take(L.slab_dx ? 4 * (size_t)L.s_dx * np * L.Hp : 0);
-        L.sdw = take(L.slab_dw ? 4 * (size_t)L.s_dw * L.piece * L.Hp : 0);
+        size_t g = (size_t)L.g_planes * np * L.piece, dbp = np / 128 * L.piece;
+        size_t sdx = L.slab_dx ? (size_t)L.s_dx * np * L.Hp : 0, sdw = L.slab_dw ? (size_t)L.s_dw * up(std::min(o.n_out, L.piece), 128) * L.Hp : 0;
+        if (most_of_fewer) {
+            // tiles x parts is at most 3/2 kFillCtas (the share of a CTA) more than the tiles, and no part is shorter than least_kb
+            auto slab = [&](long long tiles, int kb) {
+                return (size_t)std::min(tiles + 3 * kFillCtas / 2, tiles * cdiv(std::max(1, kb), least_kb)) * 128 * std::min(L.tn_products, L.Hp);
+            };
+            const long long all_dw = (long long)cdiv(o.n_out, 128) * ht;
+            sdx = slab(L.pieces > 1 ? t_dx : std::min<long long>(t_dx, kNarrowTiles), kb_dx);
+            sdw = slab(std::min<long long>(all_dw, kNarrowTiles), kb_dw);
+            const size_t whole = np * (size_t)all, limit = kLossPieceBytes / 2;
+            g = std::min((size_t)L.planes * whole, std::max(limit, (size_t)L.planes * np * 2048));
+            if (!f32) g = std::max(g, std::min<size_t>(2 * std::min(np, (size_t)256) * all, std::max(limit, 2 * std::min(np, (size_t)256) * 2048)));
+            dbp = std::min(whole, std::max(limit, np * 2048)) / 128;
+        }
+        L.next = take(4 * 2 * (size_t)(most_of_fewer ? cdiv(o.n_out, 2048) : L.pieces));
+        L.g = take(2 * g);
+        L.dbp = take(4 * dbp);
+        L.sdx = take(4 * sdx);
+        L.sdw = take(4 * sdw);
     }
     L.total = off;
     return L;
@@ -1248,6 +1363,8 @@ cudaError_t loss_run(const LossCall& c) {
     r.target = c.target; r.ids = c.ids; r.y = c.y; r.x = c.x; r.ldx = c.ldx;
     r.counts = reinterpret_cast<int32_t*>(c.ws + L.counts);
     r.mark = c.ws + L.mark;
+    r.next = reinterpret_cast<int32_t*>(c.ws + L.next);
+    r.n_next = c.grad ? 2 * L.pieces : 1;
     r.src = reinterpret_cast<int32_t*>(c.ws + L.src);
     r.target_c = reinterpret_cast<int32_t*>(c.ws + L.target);
     r.scale_c = reinterpret_cast<float*>(c.ws + L.scale);
@@ -1264,7 +1381,7 @@ cudaError_t loss_run(const LossCall& c) {
     if (r.counted) {
         if ((e = launch_small(loss_count_kernel, cdiv(c.N, ROWS_COUNTED), c.stream, r)) != cudaSuccess) return e;
     }
-    r.per_block = std::min(256, up(cdiv(c.N, 16 * sms), 8));   // a block's warps take one row each while that fills the chip
+    r.per_block = std::min(256, up(cdiv(c.N, 8 * sms), 8));   // one wave of blocks (8 an SM), while they are not too long
     r.row_blocks = cdiv(c.N, r.per_block);
     const void* w = c.o.w;
     int64_t ldw = c.o.ldw;
@@ -1300,6 +1417,7 @@ cudaError_t loss_run(const LossCall& c) {
         p.pq = reinterpret_cast<float*>(c.ws + L.pq);
         const LossLaunch l = loss_launch_of<FORWARD>(c.K > 0, L.planes);
         ring_of(p, l.a_parts, l.b_parts, few, L.tn);
+        p.next = r.next;
         if ((e = launch_gemm(l, (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
         return launch_small(loss_combine_kernel, cdiv(c.N, 8), c.stream, ctrl, r.src, p.pm, p.ps, p.pq, L.parts, L.Npad, c.K ? r.ent : nullptr, c.tau,
                             c.loss, c.lse_out);
@@ -1311,15 +1429,14 @@ cudaError_t loss_run(const LossCall& c) {
     p.ht = cdiv(c.o.H, L.tn_products); p.s_dx = L.s_dx; p.s_dw = L.s_dw;
     p.sdx = L.slab_dx ? reinterpret_cast<float*>(c.ws + L.sdx) : nullptr;
     p.sdw = L.slab_dw ? reinterpret_cast<float*>(c.ws + L.sdw) : nullptr;
-    p.slab_rows_dw = L.piece;
+    p.slab_rows_dw = up(std::min(c.o.n_out, L.piece), 128);
+    p.dx_first = cdiv(cdiv(std::min(c.o.n_out, L.piece), BK), L.s_dx) >= cdiv(L.Npad / BK, L.s_dw);
     p.dx = c.dx; p.lddx = c.lddx; p.want_dx = c.dx != nullptr; p.dx_vec = vec_rows(c.dx, c.lddx, c.o.H, f32);
     p.dw = c.dw; p.lddw = c.lddw; p.want_dw = c.dw != nullptr; p.dw_vec = vec_rows(c.dw, c.lddw, c.o.H, f32);
     if ((e = loss_map(&map_g, p.g, L.g_planes, L.Npad, L.piece, L.piece, few)) != cudaSuccess) return e;
     if ((e = loss_map(&map_g64, p.g, L.g_planes, L.Npad, L.piece, L.piece, 64)) != cudaSuccess) return e;
     if ((e = loss_map(&map_x64, r.xc, L.planes, L.Npad, L.Hp, L.Hp, 64)) != cudaSuccess) return e;
     if ((e = loss_map(&map_w64, w, L.planes, c.o.n_out, w_cols, ldw, 64)) != cudaSuccess) return e;
-    const int sum_blocks = 8 * sms;
-    const auto sum_kernel = f32 ? loss_sum_kernel<true> : loss_sum_kernel<false>;
     for (int piece = 0; piece < L.pieces; ++piece) {
         p.v0 = piece * L.piece;
         p.cols = std::min(L.piece, c.o.n_out - p.v0);
@@ -1329,26 +1446,35 @@ cudaError_t loss_run(const LossCall& c) {
         p.dbp = !c.db ? nullptr : one_tile ? c.db + p.v0 : reinterpret_cast<float*>(c.ws + L.dbp);
         const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, L.g_planes);
         ring_of(p, l.a_parts, l.b_parts, few, L.tn);
+        p.next = r.next + 2 * piece;
         if ((e = launch_gemm(l, (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
+        FinishParams f{};
+        f.ctrl = ctrl; f.H = c.o.H; f.Hp = L.Hp; f.cols = p.cols;
+        int finish_blocks = 0;
         if (c.db && !one_tile) {
-            if ((e = launch_small(loss_bias_kernel, cdiv(p.cols, 32), c.stream, ctrl, p.dbp, L.piece, p.cols, c.db + p.v0)) != cudaSuccess) return e;
+            f.dbp = p.dbp; f.ld_dbp = L.piece; f.db = c.db + p.v0;
+            finish_blocks = cdiv(p.cols, 32);
         }
-        if (!c.dx && !c.dw) continue;
         p.tn = L.tn_products;
         const LossLaunch lp = loss_launch_of<PRODUCTS>(false, L.g_planes);
         ring_of(p, lp.a_parts, lp.b_parts, c.dw ? BM : few, p.tn);
         p.a_rows = few;
         const long long units = (c.dx ? (long long)L.s_dx * row_tiles * p.ht : 0) + (c.dw ? (long long)L.s_dw * cdiv(p.cols, BM) * p.ht : 0);
-        if ((e = launch_gemm(lp, units, sms, map_g, map_w64, map_g64, map_x64, p, c.stream)) != cudaSuccess) return e;
+        p.next = r.next + 2 * piece + 1;
+        if (units && (e = launch_gemm(lp, units, sms, map_g, map_w64, map_g64, map_x64, p, c.stream)) != cudaSuccess) return e;
         if (c.dw && L.slab_dw) {
-            void* out = static_cast<uint8_t*>(c.dw) + (size_t)p.v0 * c.lddw * es;
-            if ((e = launch_small(sum_kernel, sum_blocks, c.stream, ctrl, p.sdw, L.s_dw, L.piece, p.cols, c.o.H, L.Hp, nullptr, out, c.lddw, p.dw_vec)) !=
-                cudaSuccess)
-                return e;
+            f.sdw = p.sdw; f.s_dw = L.s_dw; f.slab_rows_dw = p.slab_rows_dw;
+            f.dw = static_cast<uint8_t*>(c.dw) + (size_t)p.v0 * c.lddw * es; f.lddw = c.lddw; f.dw_vec = p.dw_vec;
+            f.blocks_dw = (int)std::min<long long>(((long long)p.cols * ((c.o.H + 3) / 4) + 255) / 256, 8LL * sms);
         }
+        if (c.dx && L.slab_dx && piece == L.pieces - 1) {
+            f.sdx = p.sdx; f.s_dx = L.s_dx; f.slab_rows_dx = L.Npad;
+            f.src = r.src; f.dx = c.dx; f.lddx = c.lddx; f.dx_vec = p.dx_vec;
+            f.blocks_dx = (int)std::min<long long>(((long long)c.N * ((c.o.H + 3) / 4) + 255) / 256, 8LL * sms);
+        }
+        finish_blocks += f.blocks_dw + f.blocks_dx;
+        if (finish_blocks && (e = launch_small(f32 ? loss_finish_kernel<true> : loss_finish_kernel<false>, finish_blocks, c.stream, f)) != cudaSuccess) return e;
     }
-    if (c.dx && L.slab_dx)
-        return launch_small(sum_kernel, sum_blocks, c.stream, ctrl, p.sdx, L.s_dx, L.Npad, 0, c.o.H, L.Hp, r.src, c.dx, c.lddx, p.dx_vec);
     return cudaSuccess;
 }
 

@@ -32,7 +32,7 @@ struct LossLayout {
     int tn_products;   // columns of a tile of dx and dW
     int s_dx, s_dw;    // parts that the sums of dx (over a piece's outputs) and dW (over the rows) are cut into
     int slab_dx, slab_dw;   // whether dx / dW go through fp32 partial sums
-    size_t ctrl, counts, mark, src, target, scale, nlse, sid, sq, ent, x, w, pm, ps, pq, g, dbp, sdx, sdw, total;
+    size_t ctrl, next, counts, mark, src, target, scale, nlse, sid, sq, ent, x, w, pm, ps, pq, g, dbp, sdx, sdw, total;
 };
 
 struct LossCall {
@@ -49,7 +49,8 @@ struct LossCall {
     cudaStream_t stream;
 };
 
-LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad);
+// most_of_fewer: `total` is the most that a call of up to N rows needs (the offsets are not to be used).
+LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most_of_fewer = false);
 cudaError_t loss_run(const LossCall& c);
 
 }  // namespace wind

@@ -43,7 +43,7 @@ def test_workspace_sizes(lib):
     assert x < size(lib, big, 4096) < x + 4096 * (65536 // 128) * 12 + (1 << 20)
     # a gradient keeps at most 512 MB of its share of logits (or 2048 outputs' worth)
     g = size(lib, big, 4096, 0, 1)
-    assert g < 2 * x + (512 << 20) + 4096 * 2048 * 4 + 32 * 65536 * 4 + (1 << 21)
+    assert g < 2 * x + (512 << 20) + (512 << 20) // 64 + 2 * 814 * 128 * 256 * 4
     rows = 1 << 20
     many = layer(n_out=65536, H=64, ldw=64)
     assert size(lib, many, rows, 0, 1) < rows * (2048 * 2 + 64 * (2 + 4) + 2048 // 128 * 4 + 64)
@@ -51,9 +51,15 @@ def test_workspace_sizes(lib):
     assert size(lib, layer(w=(1 << 20) + 2), 8) >= size(lib, layer(), 8) + 1025 * 640 * 2
     assert size(lib, layer(ldw=641), 8) >= size(lib, layer(), 8) + 1025 * 640 * 2
     assert size(lib, layer(dtype=bd.WIND_DT_F32), 8) >= size(lib, layer(), 8) + 1025 * 640 * 6
-    # more rows or entries never ask for less
-    sizes = [size(lib, layer(), N, 16, 1) for N in (0, 1, 127, 128, 129, 5000, 100000)]
-    assert sizes == sorted(sizes)
+    # what N rows need serves fewer rows and entries
+    rows_of = sorted(set([0, 1, 2, 127, 128, 129, 255, 256, 257, 384, 385, 512, 513, 8192, 8193, 20011, 32768, 32769, 100000, 1 << 20] +
+                         list(range(130, 9000, 331))))
+    for kw in (dict(), dict(n_out=33, H=64, ldw=64), dict(n_out=8193, H=1024, ldw=1024), dict(n_out=65536, H=2048, ldw=2048),
+               dict(dtype=bd.WIND_DT_F32), dict(dtype=bd.WIND_DT_F32, n_out=8193, H=1024, ldw=1024), dict(H=1, ldw=1, n_out=1)):
+        for K, grad in ((0, 0), (0, 1), (16, 0), (256, 1)):
+            sizes = [size(lib, layer(**kw), N, K, grad) for N in rows_of]
+            assert sizes == sorted(sizes), (kw, K, grad)
+            assert size(lib, layer(**kw), 777, 0, grad) <= size(lib, layer(**kw), 777, 16, grad)
 
 
 def test_calls_are_refused_before_any_launch(lib):
@@ -97,6 +103,32 @@ def test_calls_are_refused_before_any_launch(lib):
         refused(f, args, 8, None)                                   # loss, lse
     refused(lib.wind_distill_loss, dist, 9, None)
     assert lib.wind_loss_status(None, None) == bd.WIND_ERR_INVALID_ARG
+
+
+def test_reported_sizes_are_enough(lib):
+    """A workspace of the reported size is accepted by calls of as many rows and of fewer (they go on to the device, which is not there)."""
+    torch = pytest.importorskip("torch")
+    if torch.cuda.is_available():
+        pytest.skip("the calls have addresses that must not reach a device")
+    import random
+    r = random.Random(3)
+    p, ws = 1 << 20, 1 << 21
+    for _ in range(3000):
+        H, n_out = int(2 ** r.uniform(0, 12)), int(2 ** r.uniform(0, 17))
+        o = layer(H=H, ldw=H, n_out=n_out, dtype=r.choice([0, 1]))
+        N, K = int(2 ** r.uniform(0, 18)), r.choice([0, 1, 40])
+        n = max(1, min(N, int(N * r.choice([1.0, 1.0, r.random()]))))
+        ref, rows = C.byref(o), ((p, p, n, K, 1.0) if K else (p, n))
+        for grad in (0, 1):
+            have = size(lib, o, N, K, grad)
+            assert have > 0
+            if grad:
+                f = lib.wind_distill_loss_grad if K else lib.wind_label_loss_grad
+                st = f(ref, p, H, *rows, p, p, p, H, p, H, p, ws, have, None)
+            else:
+                f = lib.wind_distill_loss if K else lib.wind_label_loss
+                st = f(ref, p, H, *rows, p, p, ws, have, None)
+            assert st == bd.WIND_ERR_CUDA, (st, H, n_out, o.dtype, N, n, K, grad)
 
 
 def test_no_cpu_path(lib):
