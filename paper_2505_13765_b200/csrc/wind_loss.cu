@@ -59,7 +59,7 @@ enum Mark : uint8_t { ROW_NONE = 0, ROW_COUNTS = 1, ROW_BAD = 2 };   // BAD: a l
 
 struct RowsParams {
     LossCtrl* ctrl;
-    int N, n_out, K, H, Hp, Npad, x_vec, grad;
+    int N, n_out, K, H, Hp, Npad, x_vec, dx_vec, grad;
     int32_t* next; int n_next; // units taken by the products' kernels
     int row_blocks;            // blocks of loss_gather that take rows; those behind them lay W out
     const void* w; int64_t ldw; int w_vec; __nv_bfloat16* wc;
@@ -266,13 +266,13 @@ __device__ __forceinline__ void pack_w(const RowsParams& p, int block, int block
     }
 }
 
-// A block takes per_block rows, a warp a row at a time.  Where its first row that counts goes is the number of such rows before it,
+// A block takes per_block rows.  Where its first row that counts goes is the number of such rows before it,
 // which every block finds out for itself: reading up to ROWS_COUNTED marks from L2 is quicker than another launch.
 template <bool F32>
 __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
-    __shared__ int s_before[8], s_pos[256];
+    __shared__ int s_before[8];
     __shared__ uint32_t s_ballot[8];
-    __shared__ uint8_t s_mark[256];
+    __shared__ uint8_t s_mark[256], s_row[256];
     let_next_start();
     wait_for_previous();
     if ((int)blockIdx.x >= p.row_blocks) {
@@ -334,46 +334,62 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
     if (lane == 0) { s_before[warp] = before; s_ballot[warp] = ballot; }
     s_mark[threadIdx.x] = mine;
     bad = __syncthreads_or(bad || mine == ROW_BAD);
-    int base = 0, total = 0;
+    // s_row: the block's rows that count, in order, and behind them, from the end, the others
+    int mine_before = __popc(ballot & ((1u << lane) - 1u)), here = 0, first_pos = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        base += s_before[i] + (i < warp ? __popc(s_ballot[i]) : 0);
-        total += s_before[i] + __popc(s_ballot[i]);
+        first_pos += s_before[i];
+        here += __popc(s_ballot[i]);
+        if (i < warp) mine_before += __popc(s_ballot[i]);
     }
-    s_pos[threadIdx.x] = base + __popc(ballot & ((1u << lane) - 1u));
+    const int rows = r1 - r0, me = (int)threadIdx.x;
+    if (me < rows) {
+        if (mine == ROW_COUNTS) s_row[mine_before] = (uint8_t)me;
+        else s_row[rows - 1 - (me - mine_before)] = (uint8_t)me;
+    }
     __syncthreads();
     const size_t plane = (size_t)p.Npad * p.Hp;
     const size_t es = F32 ? 4 : 2;
-    for (int i = warp; r0 + i < r1; i += 8) {
-        const int r = r0 + i;
-        if (s_mark[i] == ROW_COUNTS) {
-            const int j = s_pos[i];
-            const uint8_t* row = static_cast<const uint8_t*>(p.x) + (size_t)r * p.ldx * es;
+    // eight columns a thread, over all rows of the block: their loads are under way together
+    const int per_row = p.Hp / 8, chunks = here * per_row;
 #pragma unroll 4
-            for (int c = lane * 8; c < p.Hp; c += 256) {
-                float v[8];
-                load8<F32>(row, c, p.H, p.x_vec, v);
-                store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, v);
-            }
-            if (lane == 0) {
-                p.src[j] = r;
-                if (p.K == 0) p.target_c[j] = p.target[r];
-                if (p.grad) {
-                    p.scale_c[j] = (p.dloss ? p.dloss[r] : 1.f) * p.tau;
-                    p.nlse_c[j] = p.lse[r];
-                }
-            }
-        } else {
-            const float fill = s_mark[i] == ROW_BAD ? CUDART_NAN_F : 0.f;
-            if (!p.grad) {
-                if (lane == 0) { p.loss[r] = fill; p.lse_out[r] = fill; }
-            } else if (p.dx) {
-                uint8_t* row = static_cast<uint8_t*>(p.dx) + (size_t)r * p.lddx * es;
+    for (int i = me; i < chunks; i += 256) {
+        const int k = i / per_row, c = (i - k * per_row) * 8;
+        float v[8];
+        load8<F32>(static_cast<const uint8_t*>(p.x) + (size_t)(r0 + s_row[k]) * p.ldx * es, c, p.H, p.x_vec, v);
+        store8<F32>(p.xc + (size_t)(first_pos + k) * p.Hp + c, plane, v);
+    }
+    if (me < here) {
+        const int r = r0 + s_row[me], j = first_pos + me;
+        p.src[j] = r;
+        if (p.K == 0) p.target_c[j] = p.target[r];
+        if (p.grad) {
+            p.scale_c[j] = (p.dloss ? p.dloss[r] : 1.f) * p.tau;
+            p.nlse_c[j] = p.lse[r];
+        }
+    }
+    if (!p.grad) {
+        if (me >= here && me < rows) {
+            const int r = s_row[me];
+            const float fill = s_mark[r] == ROW_BAD ? CUDART_NAN_F : 0.f;
+            p.loss[r0 + r] = fill;
+            p.lse_out[r0 + r] = fill;
+        }
+    } else if (p.dx) {
+        for (int k = here + warp; k < rows; k += 8) {
+            const int r = s_row[k];
+            const float fill = s_mark[r] == ROW_BAD ? CUDART_NAN_F : 0.f;
+            uint8_t* row = static_cast<uint8_t*>(p.dx) + (size_t)(r0 + r) * p.lddx * es;
+            if (p.dx_vec) {
+                const uint32_t w = F32 ? __float_as_uint(fill) : pack_bf16x2(fill, fill);
+                for (int c = lane; c < p.H * (int)es / 16; c += 32) reinterpret_cast<uint4*>(row)[c] = make_uint4(w, w, w, w);
+            } else {
                 for (int c = lane; c < p.H; c += 32) store_one<F32>(row, c, fill);
             }
         }
     }
     if ((int)blockIdx.x == p.row_blocks - 1) {
+        const int total = first_pos + here;
         // dW sums over K blocks of 64 rows: zeros behind the last one.  (Other products only make rows of it that nobody looks at.)
         if (threadIdx.x == 0) {   // (this block has seen every mark)
             p.ctrl->status = bad ? WIND_ERR_INVALID_ARG : WIND_OK;
@@ -1359,6 +1375,7 @@ cudaError_t loss_run(const LossCall& c) {
     r.ctrl = ctrl;
     r.N = c.N; r.n_out = c.o.n_out; r.K = c.K; r.H = c.o.H; r.Hp = L.Hp; r.Npad = L.Npad; r.grad = c.grad;
     r.x_vec = vec_rows(c.x, c.ldx, c.o.H, f32);
+    r.dx_vec = vec_rows(c.dx, c.lddx, c.o.H, f32);
     r.tau = c.tau;
     r.target = c.target; r.ids = c.ids; r.y = c.y; r.x = c.x; r.ldx = c.ldx;
     r.counts = reinterpret_cast<int32_t*>(c.ws + L.counts);
