@@ -9,6 +9,7 @@
 namespace wind {
 
 constexpr int kLossMaxK = 256;            // teacher's entries of a row
+constexpr int kLossMaxCtas = 256;
 constexpr int kLossMaxRows = 1 << 24;
 constexpr int kLossMaxOut = (1 << 24) - 1;
 constexpr int kLossMaxH = 1 << 16;
@@ -18,6 +19,7 @@ constexpr size_t kLossPieceBytes = (size_t)512 << 20;   // the gradient's share 
 struct LossCtrl {
     int32_t status;   // wind_status_t, first error wins
     int32_t n_rows;   // rows with a loss
+    int32_t gave_up[kLossMaxCtas];   // CTAs whose waits ran out, where nothing runs ahead of them that could reset `status`
 };
 
 // How a call is cut up, and the byte offsets of its workspace regions.  Host arithmetic on the sizes alone.

@@ -322,12 +322,13 @@ def test_same_bits_every_time(pkg, dtype, K):
 def test_labels_that_are_none(pkg, K):
     """An index outside the outputs: NaN in its row, an error status, nothing in the other rows."""
     for bad in (-2, 100, 2 ** 31 - 1, -2 ** 31):
-        c = make(71, "bf16", 200, 64, 100, K, pad=0.1, full=True)
+        N = 200 if bad % 2 == 0 else 90
+        c = make(71, "bf16", N, 64, 100, K, pad=0.1, full=True)
         ok = {k: (v.clone() if torch.is_tensor(v) else v) for k, v in c.items()}
         (c["ids"][13, 2:3] if K else c["t"][13:14]).fill_(bad)
         (ok["ids"][13] if K else ok["t"][13:14]).fill_(-1)          # as if the row were padding
         ref = reference(ok)
-        ws = pkg.alloc_loss_workspace(c["w"], 200, K, True)
+        ws = pkg.alloc_loss_workspace(c["w"], N, K, True)
         got = call(pkg, c, ws=ws, check=False)
         with pytest.raises(pkg.WindError) as e:
             pkg.wind_loss_status(ws)
