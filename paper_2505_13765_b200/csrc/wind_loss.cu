@@ -35,6 +35,7 @@
 
 #include "wind_internal.cuh"
 #include "wind_loop.cuh"
+#include "wind_loop_cl.cuh"   // cl_rank, cl_map, cl_barrier
 #include "wind_loss.cuh"
 #include "wind_ptx.cuh"
 
@@ -513,23 +514,24 @@ struct Unit {
     int part;            // PRODUCTS: which part of the sum
 };
 
-template <int MODE>
+template <int MODE, int TM>
 __device__ __forceinline__ long long count_units(const LossGemm& p, int n_rows) {
-    const int mtc = (n_rows + BM - 1) / BM;
+    const int mtc = (n_rows + TM - 1) / TM;
     if (MODE != PRODUCTS) return (long long)mtc * p.n_vt;
     long long n = 0;
     if (p.want_dx) n += (long long)p.s_dx * mtc * p.ht;
-    if (p.want_dw) n += (long long)p.s_dw * ((p.cols + BM - 1) / BM) * p.ht;
+    if (p.want_dw) n += (long long)p.s_dw * ((p.cols + TM - 1) / TM) * p.ht;
     return n;
 }
 
-// Logits: bands of LT_BAND row tiles, in a band row tile fastest, so that the CTAs at work share few tiles of x and of W; last tiles of
+// Tiles of TM rows.  Logits: bands of LT_BAND x 128 rows, in a band row tile fastest, so that the CTAs at work share few tiles of x and of W; last tiles of
 // at most half the columns (1024 labels and the blank) come behind all others.  Products: the longer ones first.  CTAs take the next
 // unit when they are through with one, and what is short at the end fills the gaps.
-template <int MODE>
+template <int MODE, int TM>
 __device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long u) {
     Unit t{};
-    const int mtc = (n_rows + BM - 1) / BM;
+    constexpr int BAND = LT_BAND * BM / TM;
+    const int mtc = (n_rows + TM - 1) / TM;
     if (MODE != PRODUCTS) {
         const int rest = p.cols - (p.n_vt - 1) * p.tn, wide = p.n_vt - (p.n_vt > 1 && 2 * rest <= p.tn);
         t.nk = p.kb;
@@ -539,17 +541,17 @@ __device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long
             t.mt = (int)(u - n_wide);
             return t;
         }
-        const long long per_band = (long long)LT_BAND * wide;
+        const long long per_band = (long long)BAND * wide;
         const int band = u < 0x7fffffff && per_band < 0x7fffffff ? (int)((uint32_t)u / (uint32_t)per_band) : (int)(u / per_band);
-        const int r = (int)(u - band * per_band), in_band = min(LT_BAND, mtc - band * LT_BAND);
+        const int r = (int)(u - band * per_band), in_band = min(BAND, mtc - band * BAND);
         t.nt = r / in_band;
-        t.mt = band * LT_BAND + (r - t.nt * in_band);
+        t.mt = band * BAND + (r - t.nt * in_band);
         return t;
     }
-    const long long n_dx = p.want_dx ? (long long)p.s_dx * mtc * p.ht : 0, n_dw = p.want_dw ? (long long)p.s_dw * ((p.cols + BM - 1) / BM) * p.ht : 0;
+    const long long n_dx = p.want_dx ? (long long)p.s_dx * mtc * p.ht : 0, n_dw = p.want_dw ? (long long)p.s_dw * ((p.cols + TM - 1) / TM) * p.ht : 0;
     t.dw = p.dx_first ? u >= n_dx : u < n_dw;
     if (t.dw == p.dx_first) u -= t.dw ? n_dx : n_dw;
-    const int tiles = (t.dw ? (p.cols + BM - 1) / BM : mtc) * p.ht;
+    const int tiles = (t.dw ? (p.cols + TM - 1) / TM : mtc) * p.ht;
     t.part = (int)(u / tiles);
     const int r = (int)(u - (long long)t.part * tiles);
     t.mt = r / p.ht;
@@ -567,13 +569,84 @@ struct UnitRing {
     uint64_t full[UNITS], empty[UNITS];
     long long unit[UNITS];
 };
-// The n-th unit behind the first, or -1: none is left, or the wait ran out.
-__device__ __forceinline__ long long next_unit(UnitRing& ring, uint32_t n, volatile int* abort_flag) {
+// ---- two CTAs on neighbouring SMs that make one tile of 256 rows (cta_group::2) ----
+// Each fetches its 128 rows of A and half the columns of B; the first one's thread issues the products, which read both shared memories
+// and write both tensor memories.  Fetches of both are counted on the first one's barriers.
+__device__ __forceinline__ void mbar_arrive_at(uint32_t addr) {   // addr: in any CTA of the cluster
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+// mbar_wait for a barrier that the other CTA arrives at
+__device__ __forceinline__ bool mbar_wait_pair(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    unsigned long long t0 = 0;
+    for (uint32_t it = 0;; ++it) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity), "r"(20000u)
+            : "memory");
+        if (ok) return true;
+        if ((it & 7u) == 7u) {
+            if (*abort_flag) return false;
+            const unsigned long long now = globaltimer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > kWaitLimitNs) { *abort_flag = 1; return false; }
+        }
+    }
+}
+__device__ __forceinline__ void tma_load_3d_pair(void* smem_dst, const CUtensorMap* tmap, int x, int y, int z, uint32_t bar) {   // bar: either CTA's
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_u32(smem_dst)),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tc_mma_bf16_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {    // arrives at that barrier of both CTAs
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t ncols) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(ncols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+
+// The n-th unit behind the first, or -1: none is left, or the wait ran out.  A pair's first CTA takes the units and leaves each in both
+// rings; both tell it when they have read one.
+template <bool PAIR>
+__device__ __forceinline__ long long next_unit(UnitRing& ring, uint32_t n, uint32_t rank, volatile int* abort_flag) {
     const uint32_t i = n % UNITS;
-    if (!mbar_wait(&ring.full[i], (n / UNITS) & 1, abort_flag)) return -1;
+    const bool there = PAIR ? mbar_wait_pair(&ring.full[i], (n / UNITS) & 1, abort_flag) : mbar_wait(&ring.full[i], (n / UNITS) & 1, abort_flag);
+    if (!there) return -1;
     const long long u = *reinterpret_cast<volatile long long*>(&ring.unit[i]);
-    mbar_arrive(&ring.empty[i]);
+    if (PAIR && rank) mbar_arrive_at(cl_map(smem_u32(&ring.empty[i]), 0));
+    else mbar_arrive(&ring.empty[i]);
     return u;
+}
+template <bool PAIR>
+__device__ __forceinline__ bool give_unit(UnitRing& ring, uint32_t n, long long u, volatile int* abort_flag) {
+    const uint32_t i = n % UNITS, parity = ((n / UNITS) & 1) ^ 1;
+    if (!(PAIR ? mbar_wait_pair(&ring.empty[i], parity, abort_flag) : mbar_wait(&ring.empty[i], parity, abort_flag))) return false;
+    *reinterpret_cast<volatile long long*>(&ring.unit[i]) = u;
+    if (PAIR) {
+        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(cl_map(smem_u32(&ring.unit[i]), 1)), "l"(u) : "memory");
+        mbar_arrive_at(cl_map(smem_u32(&ring.full[i]), 1));
+    }
+    mbar_arrive(&ring.full[i]);
+    return true;
 }
 
 template <int MODE>
@@ -731,11 +804,10 @@ __device__ __forceinline__ void logits_row(const LossGemm& p, uint32_t taddr, co
 
 // PRODUCTS epilogue of one row's columns from h0 on; zero: the sum has no term.
 template <int KIND, int CHUNKS>
-__device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, uint32_t taddr, const float* sums, int h0, int row_in_tile, int n_rows,
+__device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, uint32_t taddr, const float* sums, int h0, int row, int n_rows,
                                             bool zero) {
     constexpr bool f32 = KIND == F32;
-    const int row = t.mt * BM + row_in_tile;                       // of dx: a gathered row; of dW: an output of the piece
-    const bool there = row < (t.dw ? p.cols : n_rows);
+    const bool there = row < (t.dw ? p.cols : n_rows);             // row, of dx: a gathered row; of dW: an output of the piece
     float* slab = t.dw ? p.sdw : p.sdx;
     const int h1 = slab ? p.Hp : p.H;
     uint8_t* out = nullptr;
@@ -793,12 +865,13 @@ __device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, ui
     }
 }
 
-template <int MODE, bool LIST, int KIND>
+template <int MODE, bool LIST, int KIND, bool PAIR>
 __global__ void __launch_bounds__((Shape<MODE, KIND>::THREADS), 1)
 loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a2,
                  const __grid_constant__ CUtensorMap map_b2, const LossGemm p) {
     using S = Shape<MODE, KIND>;
     constexpr int TN = S::TN, EPI = S::EPI, A_PARTS = S::A_PARTS, B_PARTS = S::B_PARTS;
+    constexpr int TM = PAIR ? 2 * BM : BM;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], acc_full[2], acc_empty[2], drain_bar;
     __shared__ UnitRing units;
@@ -811,29 +884,34 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 
     const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
     uint8_t* smem = align_smem_1024(smem_raw);
+    const uint32_t rank = PAIR ? cl_rank() : 0, cta = PAIR ? blockIdx.x >> 1 : blockIdx.x, ctas = PAIR ? gridDim.x >> 1 : gridDim.x;   // (or pairs)
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (int s = 0; s < p.stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], EPI / 32); }
-        for (int i = 0; i < UNITS; ++i) { mbar_init(&units.full[i], 1); mbar_init(&units.empty[i], 2); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], (PAIR ? 2 : 1) * EPI / 32); }
+        for (int i = 0; i < UNITS; ++i) { mbar_init(&units.full[i], 1); mbar_init(&units.empty[i], PAIR ? 4 : 2); }
         mbar_init(&drain_bar, 1);
         fence_barrier_init();
         prefetch_tmap(&map_a); prefetch_tmap(&map_b);
         if (MODE == PRODUCTS) { prefetch_tmap(&map_a2); prefetch_tmap(&map_b2); }
     }
-    if (warp == 1) tmem_alloc(&tmem_slot, 512);
+    if (warp == 1) {
+        if (PAIR) tmem_alloc_pair(&tmem_slot, 512);
+        else tmem_alloc(&tmem_slot, 512);
+    }
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cl_barrier();
     tc_fence_after();
     const uint32_t tmem_base = tmem_slot;
     wait_for_previous();
     const int n_rows = MODE == FORWARD && p.direct ? p.direct : p.ctrl->n_rows;
-    const long long n_units = count_units<MODE>(p, n_rows);
+    const long long n_units = count_units<MODE, TM>(p, n_rows);
     // a short kernel lets the next one start at once; blocks that wait beside a long one slow it (two per cent of a text model's step)
-    if (n_units <= gridDim.x) let_next_start();
+    if (n_units <= ctas) let_next_start();
 
-    const long long first = blockIdx.x < n_units ? (long long)blockIdx.x : -1;
+    const long long first = cta < n_units ? (long long)cta : -1;
 
     if (warp == 0) {
         if (elect_one()) {
@@ -843,42 +921,46 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             bool ok = true;
             long long u = first;
             for (uint32_t n = 0; u >= 0; ++n) {
-                const int taken = p.next ? atomicAdd(p.next, 1) : (int)u;   // (there when this unit's first K blocks are under way)
+                const int taken = PAIR && rank ? 0 : p.next ? atomicAdd(p.next, 1) : (int)u;   // (there when this unit's first K blocks are under way)
                 // The next unit is handed on once the ring is full of this one: at that point nothing waits for this unit's epilogue, which
                 // waits for the answer (and empties fp32's accumulators, without which the rest could not be fetched).
                 auto hand_on = [&] {
-                    if (!mbar_wait(&units.empty[n % UNITS], ((n / UNITS) & 1) ^ 1, &abort_flag)) return false;
-                    u = (long long)gridDim.x + taken;
+                    if (PAIR && rank) {
+                        u = next_unit<PAIR>(units, n, rank, &abort_flag);
+                        return u >= 0 || !abort_flag;
+                    }
+                    u = (long long)ctas + taken;
                     if (u >= n_units) u = -1;
-                    *reinterpret_cast<volatile long long*>(&units.unit[n % UNITS]) = u;
-                    mbar_arrive(&units.full[n % UNITS]);
-                    return true;
+                    return give_unit<PAIR>(units, n, u, &abort_flag);
                 };
-                const Unit t = unit_of<MODE>(p, n_rows, u);
-                const int panels = (unit_cols<MODE>(p, t) + 63) / 64;
+                const Unit t = unit_of<MODE, TM>(p, n_rows, u);
+                // (a pair: half the columns each, 32 at least)
+                const int half = PAIR ? (unit_cols<MODE>(p, t) + 63) / 64 * 32 : 0, b0 = rank * half, row0 = t.mt * TM + rank * BM;
+                const int panels = PAIR ? (half + 63) / 64 : (unit_cols<MODE>(p, t) + 63) / 64;
                 const int a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2;
-                const uint32_t bytes = A_PARTS * a_part + B_PARTS * (MODE == PRODUCTS ? panels * PANEL_BYTES : p.tn * BK * 2);
+                const uint32_t bytes = A_PARTS * a_part + B_PARTS * (MODE == PRODUCTS ? panels * PANEL_BYTES : p.b_bytes);
                 const int hand_at = t.k0 + min(t.nk, p.stages) - 1;
                 for (int kb = t.k0; kb < t.k0 + t.nk; ++kb) {
                     if (!mbar_wait(&empty_bar[s], (turn & 1) ^ 1, &abort_flag)) { ok = false; break; }
                     uint8_t* b = a + A_PARTS * a_part;
-                    uint64_t* full = &full_bar[s];
-                    mbar_expect_tx(full, bytes);
+                    if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], PAIR ? 2 * bytes : bytes);
+                    const uint32_t full = PAIR ? cl_map(smem_u32(&full_bar[s]), 0) : 0;
+                    auto fetch = [&](uint8_t* to, const CUtensorMap* map, int x, int y, int z) {
+                        if (PAIR) tma_load_3d_pair(to, map, x, y, z, full);
+                        else tma_load_3d(to, map, x, y, z, &full_bar[s]);
+                    };
                     if (MODE != PRODUCTS) {
-                        for (int i = 0; i < A_PARTS; ++i) tma_load_3d(a + i * a_part, &map_a, kb * BK, t.mt * BM, i, full);
-                        for (int i = 0; i < B_PARTS; ++i) tma_load_3d(b + i * p.b_bytes, &map_b, kb * BK, p.v0 + t.nt * p.tn, i, full);
+                        for (int i = 0; i < A_PARTS; ++i) fetch(a + i * a_part, &map_a, kb * BK, row0, i);
+                        for (int i = 0; i < B_PARTS; ++i) fetch(b + i * p.b_bytes, &map_b, kb * BK, p.v0 + t.nt * p.tn + b0, i);
                     } else if (!t.dw) {
-                        for (int i = 0; i < A_PARTS; ++i) tma_load_3d(a + i * a_part, &map_a, kb * BK, t.mt * BM, i, full);
+                        for (int i = 0; i < A_PARTS; ++i) fetch(a + i * a_part, &map_a, kb * BK, row0, i);
                         for (int i = 0; i < B_PARTS; ++i)
-                            for (int q = 0; q < panels; ++q)
-                                tma_load_3d(b + i * p.b_bytes + q * PANEL_BYTES, &map_b, t.nt * p.tn + q * 64, p.v0 + kb * BK, i, full);
+                            for (int q = 0; q < panels; ++q) fetch(b + i * p.b_bytes + q * PANEL_BYTES, &map_b, t.nt * p.tn + b0 + q * 64, p.v0 + kb * BK, i);
                     } else {
                         for (int i = 0; i < A_PARTS; ++i)
-                            for (int q = 0; q < 2; ++q)
-                                tma_load_3d(a + i * a_part + q * PANEL_BYTES, &map_a2, t.mt * BM + q * 64, kb * BK, i, full);
+                            for (int q = 0; q < 2; ++q) fetch(a + i * a_part + q * PANEL_BYTES, &map_a2, row0 + q * 64, kb * BK, i);
                         for (int i = 0; i < B_PARTS; ++i)
-                            for (int q = 0; q < panels; ++q)
-                                tma_load_3d(b + i * p.b_bytes + q * PANEL_BYTES, &map_b2, t.nt * p.tn + q * 64, kb * BK, i, full);
+                            for (int q = 0; q < panels; ++q) fetch(b + i * p.b_bytes + q * PANEL_BYTES, &map_b2, t.nt * p.tn + b0 + q * 64, kb * BK, i);
                     }
                     a += p.stage_bytes;
                     if (++s == p.stages) { s = 0; ++turn; a = smem; }
@@ -887,7 +969,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (ok && t.nk == 0) ok = hand_on();
                 if (!ok) break;
             }
-            if (!ok) {   // given up: the copies in flight still write into this CTA's shared memory
+            if (!ok && rank == 0) {   // given up: the copies in flight still write into shared memory (of both CTAs, which leave together)
                 int late = 0;
                 for (int i = 0; i < p.stages; ++i) {
                     const uint32_t uses = turn + (i < s);        // of stage i
@@ -896,18 +978,18 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
         }
     } else if (warp == 1) {
-        if (elect_one()) {
+        if (rank == 0 && elect_one()) {
             int s = 0;
             uint32_t turn = 0, n_acc = 0, at = 0;                     // at: of stage s, in units of 16 bytes
             const uint64_t major_k = smem_desc_sw128(smem_u32(smem)), major_mn = smem_desc_mn(smem_u32(smem));
             const uint32_t stage = p.stage_bytes >> 4, b_bytes = p.b_bytes >> 4;
             bool ok = true;
             uint32_t n_unit = 0;
-            for (long long u = first; u >= 0 && ok; u = next_unit(units, n_unit++, &abort_flag)) {
-                const Unit t = unit_of<MODE>(p, n_rows, u);
-                const int n = (unit_cols<MODE>(p, t) + 31) / 32 * 32;   // (the epilogues read 32 columns at a time)
+            for (long long u = first; u >= 0 && ok; u = next_unit<PAIR>(units, n_unit++, 0, &abort_flag)) {
+                const Unit t = unit_of<MODE, TM>(p, n_rows, u);
+                const int n = PAIR ? (unit_cols<MODE>(p, t) + 63) / 64 * 64 : (unit_cols<MODE>(p, t) + 31) / 32 * 32;   // (the epilogues read 32 columns at a time)
                 const bool a_mn = MODE == PRODUCTS && t.dw, b_mn = MODE == PRODUCTS;
-                const uint32_t idesc = idesc_bf16(BM, n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+                const uint32_t idesc = idesc_bf16(TM, n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                 const uint64_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;   // 16 of K, in units of 16 bytes
                 uint32_t tm_d = 0;
                 const uint32_t a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2 >> 4;
@@ -916,7 +998,9 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     const uint32_t acc = n_acc & 1u;
                     const bool first = KIND == F32 || i == 0, last = KIND == F32 || i == t.nk - 1;   // of an accumulator
                     if (first) {
-                        if (!mbar_wait(&acc_empty[acc], ((n_acc >> 1) & 1u) ^ 1u, &abort_flag)) { ok = false; break; }
+                        const uint32_t parity = ((n_acc >> 1) & 1u) ^ 1u;
+                        ok = PAIR ? mbar_wait_pair(&acc_empty[acc], parity, &abort_flag) : mbar_wait(&acc_empty[acc], parity, &abort_flag);
+                        if (!ok) break;
                         tm_d = tmem_base + acc * TN;
                     }
                     if (!mbar_wait(&full_bar[s], turn & 1, &abort_flag)) { ok = false; break; }
@@ -926,17 +1010,26 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     for (int term = 0; term < S::TERMS; ++term) {
                         const uint64_t ad = adesc + S::a_part(term) * a_part, bd = bdesc + S::b_part(term) * b_bytes;
 #pragma unroll
-                        for (int k = 0; k < BK / 16; ++k) tc_mma_bf16(tm_d, ad + k * a_step, bd + k * b_step, idesc, !first || (term | k) != 0);
+                        for (int k = 0; k < BK / 16; ++k) {
+                            if (PAIR) tc_mma_bf16_pair(tm_d, ad + k * a_step, bd + k * b_step, idesc, !first || (term | k) != 0);
+                            else tc_mma_bf16(tm_d, ad + k * a_step, bd + k * b_step, idesc, !first || (term | k) != 0);
+                        }
                     }
-                    tc_commit(&empty_bar[s]);
+                    if (PAIR) tc_commit_pair(&empty_bar[s]);
+                    else tc_commit(&empty_bar[s]);
                     at += stage;
                     if (++s == p.stages) { s = 0; ++turn; at = 0; }
-                    if (last) { tc_commit(&acc_full[acc]); ++n_acc; }
+                    if (last) {
+                        if (PAIR) tc_commit_pair(&acc_full[acc]);
+                        else tc_commit(&acc_full[acc]);
+                        ++n_acc;
+                    }
                 }
             }
             if (!ok || *reinterpret_cast<volatile int*>(&abort_flag)) {   // given up: the products in flight still read it
                 int late = 0;
-                tc_commit(&drain_bar);
+                if (PAIR) tc_commit_pair(&drain_bar);
+                else tc_commit(&drain_bar);
                 mbar_wait(&drain_bar, 0, &late);
             }
         }
@@ -949,9 +1042,9 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         uint32_t n_acc = 0, n_tile = 0;
         bool ok = true;
         for (long long u = first; u >= 0; ++n_tile) {
-            const Unit t = unit_of<MODE>(p, n_rows, u);
+            const Unit t = unit_of<MODE, TM>(p, n_rows, u);
             const uint32_t lanes = tmem_base + my0 + ((uint32_t)(q * 32) << 16);
-            const int row = t.mt * BM + row_in_tile;
+            const int row = t.mt * TM + rank * BM + row_in_tile;
             float* bias = s_bias[n_tile & 1];
             // what the row needs besides its logits, under way while these are made
             const bool there = row < n_rows;
@@ -964,7 +1057,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             // One thread asks for the next unit, which is there before this one's accumulator is; all warps hear the same answer, so that
             // they leave together.  (A warp whose wait runs out goes on without waiting: the others still meet it at the barriers.)
-            if (et == 0) s_unit[n_tile & 1] = next_unit(units, n_tile, &abort_flag);
+            if (et == 0) s_unit[n_tile & 1] = next_unit<PAIR>(units, n_tile, rank, &abort_flag);
             __syncwarp();
             asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
             u = s_unit[n_tile & 1];
@@ -1005,13 +1098,16 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 } else if constexpr (MODE == LOGITS) {
                     logits_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, t.nt * p.tn + my0, width, row, there, scale, nlse, targets, &s_db[q][my0]);
                 } else {
-                    product_row<KIND, S::CHUNKS>(p, t, taddr, sums, t.nt * p.tn + my0, row_in_tile, n_rows, t.nk == 0);
+                    product_row<KIND, S::CHUNKS>(p, t, taddr, sums, t.nt * p.tn + my0, row, n_rows, t.nk == 0);
                 }
             }
             if (KIND != F32 && t.nk > 0) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&acc_empty[n_acc & 1u]);
+                if (lane == 0) {
+                    if (PAIR && rank) mbar_arrive_at(cl_map(smem_u32(&acc_empty[n_acc & 1u]), 0));
+                    else mbar_arrive(&acc_empty[n_acc & 1u]);
+                }
                 ++n_acc;
             }
             if constexpr (MODE == FORWARD) {
@@ -1032,16 +1128,18 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 __syncwarp();
                 asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
                 const int c = t.nt * p.tn + et;
-                if (et < p.tn && c < p.cols) p.dbp[(size_t)t.mt * p.ldg + c] = (s_db[0][et] + s_db[1][et]) + (s_db[2][et] + s_db[3][et]);
+                if (et < p.tn && c < p.cols) p.dbp[(size_t)(t.mt * (TM / BM) + rank) * p.ldg + c] = (s_db[0][et] + s_db[1][et]) + (s_db[2][et] + s_db[3][et]);
             }
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cl_barrier();     // neither leaves while the other may still reach into its shared memory
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, 512);
+        if (PAIR) tmem_dealloc_pair(tmem_base, 512);
+        else tmem_dealloc(tmem_base, 512);
     }
     if (threadIdx.x == 0) {
         if (MODE == FORWARD && p.direct) p.ctrl->gave_up[blockIdx.x] = abort_flag;      // (nobody has set the status of this call yet)
@@ -1198,6 +1296,12 @@ static int tile_cols(int row_tiles, int cols, int most) {
     return best;
 }
 
+// Two CTAs to a tile of 256 x 256 fetch a third less from L2 than a CTA to 128 x 256, and draw less power, but there are half as many
+// tiles to spread over the chip.  A text model's step (4096 rows, H = 2048, 65536 outputs): 3.50 ms against 3.65; the large vocabulary's
+// (H = 1024) is the same either way, the lattice's (H = 640) 138 us against 120.
+constexpr int kPairTiles = 2 * kFillCtas, kPairH = 1536;
+static bool pairs_pay(int H, long long tiles) { return H >= kPairH && tiles >= kPairTiles; }
+
 LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most_of_fewer) {
     LossLayout L{};
     const bool f32 = o.dtype == WIND_DT_F32;
@@ -1205,7 +1309,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
     L.g_planes = f32 ? 3 : N <= 256 ? 2 : 1;
     L.pack_w = f32 || o.H % 8 || o.ldw % 8 || (o.n_out > 1 && o.ldw < o.H) || reinterpret_cast<uintptr_t>(o.w) % 16;
     L.Hp = up(o.H, 64);
-    L.Npad = up(N, 128);
+    L.Npad = N <= BM ? up(N, BM) : up(N, 2 * BM);
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t at = off; off = align_up(off + bytes); return at; };
     L.ctrl = take(sizeof(LossCtrl));
@@ -1224,6 +1328,8 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
     L.w = take(L.pack_w ? 2 * (size_t)L.planes * o.n_out * L.Hp : 0);
     if (!grad) {
         L.tn = tile_cols(L.Npad / BM, o.n_out, most);
+        L.pair = !f32 && pairs_pay(o.H, (long long)(L.Npad / BM) * cdiv(o.n_out, 256));
+        if (L.pair) L.tn = most;
         L.parts = cdiv(o.n_out, L.tn);
         L.next = take(4);
         size_t parts = (size_t)L.parts * np;
@@ -1239,9 +1345,12 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
         L.piece = (int)std::min(all, std::max(2048LL, fit));
         L.pieces = cdiv(o.n_out, L.piece);
         L.tn = tile_cols(L.Npad / BM, std::min(o.n_out, L.piece), most);
+        L.pair = L.g_planes == 1 && pairs_pay(o.H, (long long)(L.Npad / BM) * cdiv(std::min(o.n_out, L.piece), 256));
+        if (L.pair) L.tn = most;
         L.tn_products = most;
         const int ht = cdiv(o.H, L.tn_products), terms = f32 ? 6 : 1;
-        const long long t_dx = (long long)(L.Npad / 128) * ht, t_dw = (long long)cdiv(std::min(o.n_out, L.piece), 128) * ht;
+        const long long t_dx = (long long)(L.Npad / BM) * ht, t_dw = (long long)cdiv(std::min(o.n_out, L.piece), BM) * ht;
+        L.pair_products = L.g_planes == 1 && pairs_pay(o.H, t_dx + t_dw);
         const int kb_dx = cdiv(std::min(o.n_out, L.piece), BK), kb_dw = L.Npad / BK;
         // Parts of a sum: units of at most two thirds of a CTA's share of all K blocks, so that the units taken last fill the gaps, but of
         // 8 K blocks (bf16) at least, and none where the tiles alone are many.
@@ -1308,19 +1417,19 @@ static cudaError_t loss_map(CUtensorMap* map, const void* base, uint64_t planes,
 
 typedef void (*LossKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const LossGemm);
 
-template <int MODE, int KIND>
+template <int MODE, int KIND, bool PAIR>
 static LossKernel loss_kernel_of(bool list) {
-    return list && MODE != PRODUCTS ? loss_gemm_kernel<MODE, MODE != PRODUCTS, KIND> : loss_gemm_kernel<MODE, false, KIND>;
+    return list && MODE != PRODUCTS ? loss_gemm_kernel<MODE, MODE != PRODUCTS, KIND, PAIR> : loss_gemm_kernel<MODE, false, KIND, PAIR>;
 }
-struct LossLaunch { LossKernel kernel; int threads, a_parts, b_parts; };
+struct LossLaunch { LossKernel kernel; int threads, a_parts, b_parts, pair; };
 template <int MODE>
-static LossLaunch loss_launch_of(bool list, int kind) {
-    if (kind == F32) return {loss_kernel_of<MODE, F32>(list), Shape<MODE, F32>::THREADS, Shape<MODE, F32>::A_PARTS, Shape<MODE, F32>::B_PARTS};
+static LossLaunch loss_launch_of(bool list, int kind, bool pair) {
+    if (kind == F32) return {loss_kernel_of<MODE, F32, false>(list), Shape<MODE, F32>::THREADS, Shape<MODE, F32>::A_PARTS, Shape<MODE, F32>::B_PARTS, 0};
     if (MODE != FORWARD && kind == BF16_FINE) {
         constexpr int M = MODE == FORWARD ? LOGITS : MODE;
-        return {loss_kernel_of<M, BF16_FINE>(list), Shape<M, BF16_FINE>::THREADS, Shape<M, BF16_FINE>::A_PARTS, Shape<M, BF16_FINE>::B_PARTS};
+        return {loss_kernel_of<M, BF16_FINE, false>(list), Shape<M, BF16_FINE>::THREADS, Shape<M, BF16_FINE>::A_PARTS, Shape<M, BF16_FINE>::B_PARTS, 0};
     }
-    return {loss_kernel_of<MODE, BF16>(list), Shape<MODE, BF16>::THREADS, Shape<MODE, BF16>::A_PARTS, Shape<MODE, BF16>::B_PARTS};
+    return {pair ? loss_kernel_of<MODE, BF16, true>(list) : loss_kernel_of<MODE, BF16, false>(list), Shape<MODE, BF16>::THREADS, 1, 1, pair};
 }
 
 // Shared-memory opt-in of the kernels of this file.
@@ -1333,8 +1442,8 @@ static cudaError_t loss_set_attributes() {
     std::lock_guard<std::mutex> lock(g_loss_mutex);
     if (done_on[dev]) return cudaSuccess;
     for (int list = 0; list < 2; ++list)
-        for (int kind = BF16; kind <= F32; ++kind)
-            for (const LossLaunch& l : {loss_launch_of<FORWARD>(list, kind), loss_launch_of<LOGITS>(list, kind), loss_launch_of<PRODUCTS>(list, kind)})
+        for (int kind = 0; kind <= F32; ++kind)      // (0: bf16 in pairs)
+            for (const LossLaunch& l : {loss_launch_of<FORWARD>(list, kind, !kind), loss_launch_of<LOGITS>(list, kind, !kind), loss_launch_of<PRODUCTS>(list, kind, !kind)})
                 if ((e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + 1024)) != cudaSuccess) return e;
     done_on[dev] = true;
     return cudaSuccess;
@@ -1358,17 +1467,28 @@ static cudaError_t launch_small(void (*kernel)(Params...), int blocks, cudaStrea
 // The ring of K blocks in shared memory.  A stage holds what is fetched: a_rows rows of A (few, where the call has few: the products
 // read 128, and what lies behind the a_rows makes rows of the result that nobody looks at) and a tile's columns of B.  A call of one
 // row has 16 K blocks of 64 columns under way instead of four.
-static void ring_of(LossGemm& p, int a_parts, int b_parts, int a_rows, int tn) {
+static void ring_of(LossGemm& p, const LossLaunch& l, int a_rows, int tn) {
     p.a_rows = a_rows;
-    p.b_bytes = tn * BK * 2;
-    p.stage_bytes = a_parts * a_rows * BK * 2 + b_parts * p.b_bytes;
+    p.b_bytes = (l.pair ? tn / 2 : tn) * BK * 2;
+    p.stage_bytes = l.a_parts * a_rows * BK * 2 + l.b_parts * p.b_bytes;
     p.stages = std::min(kMaxStages, (kRingBytes - A_STAGE_BYTES) / p.stage_bytes);
 }
 
 static cudaError_t launch_gemm(const LossLaunch& l, long long units, int sms, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& a2,
                                const CUtensorMap& b2, const LossGemm& p, cudaStream_t stream) {
     void* args[5] = {(void*)&a, (void*)&b, (void*)&a2, (void*)&b2, (void*)&p};
-    return launch_overlapped((const void*)l.kernel, dim3((unsigned)std::min<long long>(units, sms)), dim3(l.threads), args, kRingBytes + 1024, stream);
+    if (!l.pair)
+        return launch_overlapped((const void*)l.kernel, dim3((unsigned)std::min<long long>(units, sms)), dim3(l.threads), args, kRingBytes + 1024, stream);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2 * (unsigned)std::min<long long>(units, sms / 2)); cfg.blockDim = dim3(l.threads); cfg.dynamicSmemBytes = kRingBytes + 1024; cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelExC(&cfg, (const void*)l.kernel, args);
 }
 
 cudaError_t loss_run(const LossCall& c) {
@@ -1453,18 +1573,19 @@ cudaError_t loss_run(const LossCall& c) {
     if (direct) e = loss_map(&map_x, c.x, 1, c.N, c.o.H, c.N == 1 ? c.o.H : c.ldx, few);
     else e = loss_map(&map_x, r.xc, L.planes, L.Npad, L.Hp, L.Hp, few);
     if (e != cudaSuccess) return e;
-    if ((e = loss_map(&map_w, w, L.planes, c.o.n_out, w_cols, ldw, L.tn)) != cudaSuccess) return e;
+    if ((e = loss_map(&map_w, w, L.planes, c.o.n_out, w_cols, ldw, L.pair ? L.tn / 2 : L.tn)) != cudaSuccess) return e;
     const int row_tiles = L.Npad / BM;
+    const long long logit_rows = L.pair ? row_tiles / 2 : row_tiles;    // tiles
     if (!c.grad) {
         p.v0 = 0; p.cols = c.o.n_out; p.n_vt = cdiv(c.o.n_out, L.tn);
         p.pm = reinterpret_cast<float*>(c.ws + L.pm);
         p.ps = reinterpret_cast<float*>(c.ws + L.ps);
         p.pq = reinterpret_cast<float*>(c.ws + L.pq);
-        const LossLaunch l = loss_launch_of<FORWARD>(c.K > 0, L.planes);
-        ring_of(p, l.a_parts, l.b_parts, few, L.tn);
+        const LossLaunch l = loss_launch_of<FORWARD>(c.K > 0, L.planes, L.pair);
+        ring_of(p, l, few, L.tn);
         p.next = direct ? nullptr : r.next;
         if (direct) { p.direct = c.N; p.src = nullptr; p.target = c.target; }
-        if ((e = launch_gemm(l, (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
+        if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
         CombineParams q{};
         q.ctrl = ctrl; q.src = r.src; q.pm = p.pm; q.ps = p.ps; q.pq = p.pq; q.parts = L.parts; q.Npad = L.Npad;
         q.ent = c.K ? r.ent : nullptr; q.tau = c.tau; q.loss = c.loss; q.lse = c.lse_out;
@@ -1493,10 +1614,10 @@ cudaError_t loss_run(const LossCall& c) {
         p.n_vt = cdiv(p.cols, L.tn);
         p.add_dx = piece > 0;
         p.dbp = !c.db ? nullptr : one_tile ? c.db + p.v0 : reinterpret_cast<float*>(c.ws + L.dbp);
-        const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, L.g_planes);
-        ring_of(p, l.a_parts, l.b_parts, few, L.tn);
+        const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, L.g_planes, L.pair);
+        ring_of(p, l, few, L.tn);
         p.next = r.next + 2 * piece;
-        if ((e = launch_gemm(l, (long long)row_tiles * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
+        if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
         FinishParams f{};
         f.ctrl = ctrl; f.H = c.o.H; f.Hp = L.Hp; f.cols = p.cols;
         int finish_blocks = 0;
@@ -1505,10 +1626,11 @@ cudaError_t loss_run(const LossCall& c) {
             finish_blocks = cdiv(p.cols, 32);
         }
         p.tn = L.tn_products;
-        const LossLaunch lp = loss_launch_of<PRODUCTS>(false, L.g_planes);
-        ring_of(p, lp.a_parts, lp.b_parts, c.dw ? BM : few, p.tn);
+        const LossLaunch lp = loss_launch_of<PRODUCTS>(false, L.g_planes, L.pair_products);
+        ring_of(p, lp, c.dw ? BM : few, p.tn);
         p.a_rows = few;
-        const long long units = (c.dx ? (long long)L.s_dx * row_tiles * p.ht : 0) + (c.dw ? (long long)L.s_dw * cdiv(p.cols, BM) * p.ht : 0);
+        const int tm = lp.pair ? 2 * BM : BM;
+        const long long units = (c.dx ? (long long)L.s_dx * (L.Npad / tm) * p.ht : 0) + (c.dw ? (long long)L.s_dw * cdiv(p.cols, tm) * p.ht : 0);
         p.next = r.next + 2 * piece + 1;
         if (units && (e = launch_gemm(lp, units, sms, map_g, map_w64, map_g64, map_x64, p, c.stream)) != cudaSuccess) return e;
         if (c.dw && L.slab_dw) {

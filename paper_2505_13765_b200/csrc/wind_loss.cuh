@@ -32,6 +32,7 @@ struct LossLayout {
     int pieces;
     int tn, parts;     // columns of a tile of logits; partial results of a row (loss)
     int tn_products;   // columns of a tile of dx and dW
+    int pair, pair_products;   // whether two CTAs make a tile, of logits and of dx and dW
     int s_dx, s_dw;    // parts that the sums of dx (over a piece's outputs) and dW (over the rows) are cut into
     int slab_dx, slab_dw;   // whether dx / dW go through fp32 partial sums
     size_t ctrl, next, counts, mark, src, target, scale, nlse, sid, sq, ent, x, w, pm, ps, pq, g, dbp, sdx, sdw, total;

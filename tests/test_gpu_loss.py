@@ -158,12 +158,22 @@ SHAPES = [  # N, H, V: around the sizes of tiles, bands and pieces
     (128, 64, 256), (129, 64, 257), (130, 250, 300), (200, 640, 1025), (257, 264, 511), (1000, 136, 1500), (2300, 320, 700), (77, 1024, 8193),
     (4099, 64, 33),
 ]
+LARGE = [  # enough tiles that two CTAs make one; odd numbers of row tiles, last tiles of a column or of a few columns of H
+    (1700, 1640, 5377), (9100, 1544, 1025), (900, 2048, 12289), (20000, 8, 500), (2990, 640, 4097),
+]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N,H,V", SHAPES)
 def test_label_loss_and_gradient(pkg, dtype, N, H, V):
     c = make(N + H + V, dtype, N, H, V, bias=(N + V) % 3 != 0, pad=0.25 if N > 2 else 0.0)
+    verify(call(pkg, c), reference(c))
+
+
+@pytest.mark.parametrize("N,H,V", LARGE)
+@pytest.mark.parametrize("K", [0, 9])
+def test_large_calls(pkg, N, H, V, K):
+    c = make(N + H + V + K, "bf16", N, H, V, K, bias=N % 3 != 0, pad=0.1)
     verify(call(pkg, c), reference(c))
 
 
