@@ -507,8 +507,8 @@ __device__ __forceinline__ float pick32(const float* v, int at) {
 }
 
 // What a CTA's roles need to know about a piece of work.
-struct Unit {
-    int mt, nt;          // row tile of A, column tile of B
+struct __align__(8) Unit {
+    int mt, nt;          // row tile of A, column tile of B; mt -1: there is none
     int k0, nk;          // K blocks
     int dw;              // PRODUCTS: dW (else dx)
     int part;            // PRODUCTS: which part of the sum
@@ -527,48 +527,76 @@ __device__ __forceinline__ long long count_units(const LossGemm& p, int n_rows) 
 // Tiles of TM rows.  Logits: bands of LT_BAND x 128 rows, in a band row tile fastest, so that the CTAs at work share few tiles of x and of W; last tiles of
 // at most half the columns (1024 labels and the blank) come behind all others.  Products: the longer ones first.  CTAs take the next
 // unit when they are through with one, and what is short at the end fills the gaps.
-template <int MODE, int TM>
-__device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long u) {
+template <int MODE, int TM, typename Int>
+__device__ __forceinline__ Unit unit_at(const LossGemm& p, int n_rows, Int u) {
     Unit t{};
     constexpr int BAND = LT_BAND * BM / TM;
     const int mtc = (n_rows + TM - 1) / TM;
     if (MODE != PRODUCTS) {
         const int rest = p.cols - (p.n_vt - 1) * p.tn, wide = p.n_vt - (p.n_vt > 1 && 2 * rest <= p.tn);
         t.nk = p.kb;
-        const long long n_wide = (long long)mtc * wide;
+        const Int n_wide = (Int)mtc * wide;
         if (u >= n_wide) {
             t.nt = wide;
             t.mt = (int)(u - n_wide);
             return t;
         }
-        const long long per_band = (long long)BAND * wide;
-        const int band = u < 0x7fffffff && per_band < 0x7fffffff ? (int)((uint32_t)u / (uint32_t)per_band) : (int)(u / per_band);
+        const Int per_band = (Int)BAND * wide;
+        const int band = (int)(u / per_band);
         const int r = (int)(u - band * per_band), in_band = min(BAND, mtc - band * BAND);
-        t.nt = r / in_band;
+        t.nt = in_band == BAND ? r / BAND : r / in_band;
         t.mt = band * BAND + (r - t.nt * in_band);
         return t;
     }
-    const long long n_dx = p.want_dx ? (long long)p.s_dx * mtc * p.ht : 0, n_dw = p.want_dw ? (long long)p.s_dw * ((p.cols + TM - 1) / TM) * p.ht : 0;
+    const Int n_dx = p.want_dx ? (Int)p.s_dx * mtc * p.ht : 0, n_dw = p.want_dw ? (Int)p.s_dw * ((p.cols + TM - 1) / TM) * p.ht : 0;
     t.dw = p.dx_first ? u >= n_dx : u < n_dw;
     if (t.dw == p.dx_first) u -= t.dw ? n_dx : n_dw;
     const int tiles = (t.dw ? (p.cols + TM - 1) / TM : mtc) * p.ht;
     t.part = (int)(u / tiles);
-    const int r = (int)(u - (long long)t.part * tiles);
+    const int r = (int)(u - (Int)t.part * tiles);
     t.mt = r / p.ht;
     t.nt = r - t.mt * p.ht;
     const int kb = ((t.dw ? n_rows : p.cols) + BK - 1) / BK, s = t.dw ? p.s_dw : p.s_dx;
-    t.k0 = (int)((long long)kb * t.part / s);
-    t.nk = (int)((long long)kb * (t.part + 1) / s) - t.k0;
+    if (s > 1) {
+        t.k0 = (int)((long long)kb * t.part / s);
+        t.nk = (int)((long long)kb * (t.part + 1) / s) - t.k0;
+    } else {
+        t.nk = kb;
+    }
     return t;
+}
+// (divisions of 64 bits take a thousand cycles, which at the start of a kernel nothing hides)
+template <int MODE, int TM>
+__device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long u, long long n_units) {
+    if (u < 0 || u >= n_units) {
+        Unit none{};
+        none.mt = -1;
+        return none;
+    }
+    return n_units < 0x7fffffff ? unit_at<MODE, TM, uint32_t>(p, n_rows, (uint32_t)u) : unit_at<MODE, TM, long long>(p, n_rows, u);
 }
 
 // A CTA's first unit is that of its number; the others are handed on through a ring, by the one thread that fetches operands and
-// takes them, to the one that issues the products and to the epilogue.
+// takes them, to the one that issues the products and to the epilogue.  They go as tiles, worked out while earlier operands are under
+// way: left to the issuing thread, that stood 1200 cycles between one tile's products and the next one's.
 constexpr int UNITS = 4;
 struct UnitRing {
     uint64_t full[UNITS], empty[UNITS];
-    long long unit[UNITS];
+    Unit unit[UNITS];
 };
+__device__ __forceinline__ Unit read_unit(const Unit* at) {
+    const volatile long long* w = reinterpret_cast<const volatile long long*>(at);
+    long long v[3] = {w[0], w[1], w[2]};
+    Unit t;
+    memcpy(&t, v, sizeof(t));
+    return t;
+}
+__device__ __forceinline__ void write_unit(Unit* at, const Unit& t) {
+    long long v[3];
+    memcpy(v, &t, sizeof(t));
+    volatile long long* w = reinterpret_cast<volatile long long*>(at);
+    w[0] = v[0]; w[1] = v[1]; w[2] = v[2];
+}
 // ---- two CTAs on neighbouring SMs that make one tile of 256 rows (cta_group::2) ----
 // Each fetches its 128 rows of A and half the columns of B; the first one's thread issues the products, which read both shared memories
 // and write both tensor memories.  Fetches of both are counted on the first one's barriers.
@@ -624,25 +652,31 @@ __device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
 }
 
-// The n-th unit behind the first, or -1: none is left, or the wait ran out.  A pair's first CTA takes the units and leaves each in both
-// rings; both tell it when they have read one.
+// The n-th unit behind the first; mt is -1 where none is left, or the wait ran out.  A pair's first CTA takes the units and leaves each in
+// both rings; both tell it when they have read one.
 template <bool PAIR>
-__device__ __forceinline__ long long next_unit(UnitRing& ring, uint32_t n, uint32_t rank, volatile int* abort_flag) {
+__device__ __forceinline__ Unit next_unit(UnitRing& ring, uint32_t n, uint32_t rank, volatile int* abort_flag) {
     const uint32_t i = n % UNITS;
     const bool there = PAIR ? mbar_wait_pair(&ring.full[i], (n / UNITS) & 1, abort_flag) : mbar_wait(&ring.full[i], (n / UNITS) & 1, abort_flag);
-    if (!there) return -1;
-    const long long u = *reinterpret_cast<volatile long long*>(&ring.unit[i]);
+    Unit t{};
+    t.mt = -1;
+    if (!there) return t;
+    t = read_unit(&ring.unit[i]);
     if (PAIR && rank) mbar_arrive_at(cl_map(smem_u32(&ring.empty[i]), 0));
     else mbar_arrive(&ring.empty[i]);
-    return u;
+    return t;
 }
 template <bool PAIR>
-__device__ __forceinline__ bool give_unit(UnitRing& ring, uint32_t n, long long u, volatile int* abort_flag) {
+__device__ __forceinline__ bool give_unit(UnitRing& ring, uint32_t n, const Unit& t, volatile int* abort_flag) {
     const uint32_t i = n % UNITS, parity = ((n / UNITS) & 1) ^ 1;
     if (!(PAIR ? mbar_wait_pair(&ring.empty[i], parity, abort_flag) : mbar_wait(&ring.empty[i], parity, abort_flag))) return false;
-    *reinterpret_cast<volatile long long*>(&ring.unit[i]) = u;
+    write_unit(&ring.unit[i], t);
     if (PAIR) {
-        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(cl_map(smem_u32(&ring.unit[i]), 1)), "l"(u) : "memory");
+        long long v[3];
+        memcpy(v, &t, sizeof(t));
+        const uint32_t far = cl_map(smem_u32(&ring.unit[i]), 1);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(far + 8 * k), "l"(v[k]) : "memory");
         mbar_arrive_at(cl_map(smem_u32(&ring.full[i]), 1));
     }
     mbar_arrive(&ring.full[i]);
@@ -761,10 +795,12 @@ __device__ __forceinline__ float column_sums(float* v, int lane) {
 }
 
 // LOGITS epilogue of one row's columns: g, to the next multiple of 64 outputs (K blocks of the product behind), and the warp's share of
-// the columns' sums.
+// the columns' sums.  bf16: of each 32 columns the first 16 go through 1 KB of shared memory (`stage`; its 16-byte halves swizzled as the
+// tensor map says) and out by TMA, the others from registers.  All from registers, 32 rows an instruction, kept the load/store unit busy
+// for 4000 cycles a tile; all by TMA, the warp waited for its 1 KB four times a tile (a tile's epilogue: 8600 and 6700 cycles).
 template <bool LIST, int KIND, int CHUNKS>
-__device__ __forceinline__ void logits_row(const LossGemm& p, uint32_t taddr, const float* sums, const float* bias, int g_col, int n_cols, int row,
-                                           bool there, float scale, float nlse, Targets<LIST>& targets, float* col_sums) {
+__device__ __forceinline__ void logits_row(const LossGemm& p, const CUtensorMap* map_g, uint8_t* stage, uint32_t taddr, const float* sums, const float* bias,
+                                           int g_col, int n_cols, int row, bool there, float scale, float nlse, Targets<LIST>& targets, float* col_sums) {
     const int lane = threadIdx.x & 31, col = p.v0 + g_col;
     __nv_bfloat16* dst = p.g + (size_t)row * p.ldg + g_col;
     const int g_end = (p.cols + 63) / 64 * 64 - g_col;
@@ -792,8 +828,29 @@ __device__ __forceinline__ void logits_row(const LossGemm& p, uint32_t taddr, co
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
         }
+        if constexpr (KIND == BF16) {
+            const uint32_t at = smem_u32(stage) + lane * 32, swap = (lane & 4) << 2;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 32; i += 16) store16<KIND>(dst + c * 32 + i, p.g_plane, v + i);
+            for (int k = 0; k < 2; ++k)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((16u * k) ^ swap)), "r"(pack_bf16x2(v[8 * k], v[8 * k + 1])),
+                             "r"(pack_bf16x2(v[8 * k + 2], v[8 * k + 3])), "r"(pack_bf16x2(v[8 * k + 4], v[8 * k + 5])),
+                             "r"(pack_bf16x2(v[8 * k + 6], v[8 * k + 7]))
+                             : "memory");
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(map_g)),
+                             "r"(g_col + c * 32), "r"(row), "r"(smem_u32(stage))
+                             : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+            store16<1>(dst + c * 32 + 16, 0, v + 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 16) store16<KIND>(dst + c * 32 + i, p.g_plane, v + i);
+        }
         if (p.dbp) {
             __syncwarp();
             const float sum = column_sums(v, lane);
@@ -877,10 +934,10 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     __shared__ UnitRing units;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
-    __shared__ long long s_unit[2];
+    __shared__ Unit s_unit[2];
     __shared__ __align__(16) float s_bias[2][TN];
+    __shared__ float s_db[MODE == LOGITS ? 4 : 1][TN];                 // [lane quadrant][column of the tile]
     __shared__ float s_part[MODE == FORWARD ? S::GROUPS : 1][3][BM];   // [group][maximum, sum, targets' logits][row]
-    __shared__ float s_db[MODE == LOGITS ? 4 : 1][TN];     // [lane quadrant][column of the tile]
 
     const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
     uint8_t* smem = align_smem_1024(smem_raw);
@@ -894,7 +951,8 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         mbar_init(&drain_bar, 1);
         fence_barrier_init();
         prefetch_tmap(&map_a); prefetch_tmap(&map_b);
-        if (MODE == PRODUCTS) { prefetch_tmap(&map_a2); prefetch_tmap(&map_b2); }
+        if (MODE != FORWARD) prefetch_tmap(&map_a2);
+        if (MODE == PRODUCTS) prefetch_tmap(&map_b2);
     }
     if (warp == 1) {
         if (PAIR) tmem_alloc_pair(&tmem_slot, 512);
@@ -911,7 +969,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // a short kernel lets the next one start at once; blocks that wait beside a long one slow it (two per cent of a text model's step)
     if (n_units <= ctas) let_next_start();
 
-    const long long first = cta < n_units ? (long long)cta : -1;
+    const Unit first = unit_of<MODE, TM>(p, n_rows, cta, n_units);
 
     if (warp == 0) {
         if (elect_one()) {
@@ -919,27 +977,26 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             uint32_t turn = 0;       // of the ring: stage s is used for the (turn + 1)-th time
             uint8_t* a = smem;       // of stage s
             bool ok = true;
-            long long u = first;
-            for (uint32_t n = 0; u >= 0; ++n) {
-                const int taken = PAIR && rank ? 0 : p.next ? atomicAdd(p.next, 1) : (int)u;   // (there when this unit's first K blocks are under way)
+            Unit t = first;
+            for (uint32_t n = 0; t.mt >= 0; ++n) {
+                const int taken = PAIR && rank ? 0 : p.next ? atomicAdd(p.next, 1) : (int)(n * ctas + cta);   // (there when this unit's first K blocks are under way)
                 // The next unit is handed on once the ring is full of this one: at that point nothing waits for this unit's epilogue, which
                 // waits for the answer (and empties fp32's accumulators, without which the rest could not be fetched).
+                Unit then{};
                 auto hand_on = [&] {
                     if (PAIR && rank) {
-                        u = next_unit<PAIR>(units, n, rank, &abort_flag);
-                        return u >= 0 || !abort_flag;
+                        then = next_unit<PAIR>(units, n, rank, &abort_flag);
+                        return then.mt >= 0 || !abort_flag;
                     }
-                    u = (long long)ctas + taken;
-                    if (u >= n_units) u = -1;
-                    return give_unit<PAIR>(units, n, u, &abort_flag);
+                    then = unit_of<MODE, TM>(p, n_rows, (long long)ctas + taken, n_units);
+                    return give_unit<PAIR>(units, n, then, &abort_flag);
                 };
-                const Unit t = unit_of<MODE, TM>(p, n_rows, u);
                 // (a pair: half the columns each, 32 at least)
                 const int half = PAIR ? (unit_cols<MODE>(p, t) + 63) / 64 * 32 : 0, b0 = rank * half, row0 = t.mt * TM + rank * BM;
                 const int panels = PAIR ? (half + 63) / 64 : (unit_cols<MODE>(p, t) + 63) / 64;
                 const int a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2;
                 const uint32_t bytes = A_PARTS * a_part + B_PARTS * (MODE == PRODUCTS ? panels * PANEL_BYTES : p.b_bytes);
-                const int hand_at = t.k0 + min(t.nk, p.stages) - 1;
+                const int hand_at = PAIR && rank ? -1 : t.k0 + min(t.nk, p.stages) - 1;   // (the pair's other CTA hears of it when it is through)
                 for (int kb = t.k0; kb < t.k0 + t.nk; ++kb) {
                     if (!mbar_wait(&empty_bar[s], (turn & 1) ^ 1, &abort_flag)) { ok = false; break; }
                     uint8_t* b = a + A_PARTS * a_part;
@@ -966,8 +1023,9 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     if (++s == p.stages) { s = 0; ++turn; a = smem; }
                     if (kb == hand_at && !hand_on()) { ok = false; break; }
                 }
-                if (ok && t.nk == 0) ok = hand_on();
+                if (ok && (t.nk == 0 || (PAIR && rank))) ok = hand_on();
                 if (!ok) break;
+                t = then;
             }
             if (!ok && rank == 0) {   // given up: the copies in flight still write into shared memory (of both CTAs, which leave together)
                 int late = 0;
@@ -985,8 +1043,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint32_t stage = p.stage_bytes >> 4, b_bytes = p.b_bytes >> 4;
             bool ok = true;
             uint32_t n_unit = 0;
-            for (long long u = first; u >= 0 && ok; u = next_unit<PAIR>(units, n_unit++, 0, &abort_flag)) {
-                const Unit t = unit_of<MODE, TM>(p, n_rows, u);
+            for (Unit t = first; t.mt >= 0 && ok; t = next_unit<PAIR>(units, n_unit++, 0, &abort_flag)) {
                 const int n = PAIR ? (unit_cols<MODE>(p, t) + 63) / 64 * 64 : (unit_cols<MODE>(p, t) + 31) / 32 * 32;   // (the epilogues read 32 columns at a time)
                 const bool a_mn = MODE == PRODUCTS && t.dw, b_mn = MODE == PRODUCTS;
                 const uint32_t idesc = idesc_bf16(TM, n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
@@ -1041,8 +1098,10 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const int my0 = group * width;                     // first column of this warp's, in the tile
         uint32_t n_acc = 0, n_tile = 0;
         bool ok = true;
-        for (long long u = first; u >= 0; ++n_tile) {
-            const Unit t = unit_of<MODE, TM>(p, n_rows, u);
+        uint8_t* stage = smem + (kRingBytes - A_STAGE_BYTES) + (warp - 2) * 1024;   // (LOGITS of bf16: its A is never short)
+        Unit then = first;
+        for (; then.mt >= 0; ++n_tile) {
+            const Unit t = then;
             const uint32_t lanes = tmem_base + my0 + ((uint32_t)(q * 32) << 16);
             const int row = t.mt * TM + rank * BM + row_in_tile;
             float* bias = s_bias[n_tile & 1];
@@ -1057,10 +1116,10 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             // One thread asks for the next unit, which is there before this one's accumulator is; all warps hear the same answer, so that
             // they leave together.  (A warp whose wait runs out goes on without waiting: the others still meet it at the barriers.)
-            if (et == 0) s_unit[n_tile & 1] = next_unit<PAIR>(units, n_tile, rank, &abort_flag);
+            if (et == 0) write_unit(&s_unit[n_tile & 1], next_unit<PAIR>(units, n_tile, rank, &abort_flag));
             __syncwarp();
             asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
-            u = s_unit[n_tile & 1];
+            then = read_unit(&s_unit[n_tile & 1]);
             // fp32: an accumulator takes one K block, whose sum is added up here.  (Tensor cores cut where they add; over a long K that
             // is an error of 2^-25 an addition, all one way: 5e-6 of dW over 20 000 rows.)
             float sums[KIND == F32 ? S::CHUNKS * 32 : 1];
@@ -1096,7 +1155,8 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if constexpr (MODE == FORWARD) {
                     part = forward_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, col, min(width, p.n_out - col), targets);
                 } else if constexpr (MODE == LOGITS) {
-                    logits_row<LIST, KIND, S::CHUNKS>(p, taddr, sums, bias + my0, t.nt * p.tn + my0, width, row, there, scale, nlse, targets, &s_db[q][my0]);
+                    logits_row<LIST, KIND, S::CHUNKS>(p, &map_a2, stage, taddr, sums, bias + my0, t.nt * p.tn + my0, width, row, there, scale, nlse, targets,
+                                                      &s_db[q][my0]);
                 } else {
                     product_row<KIND, S::CHUNKS>(p, t, taddr, sums, t.nt * p.tn + my0, row, n_rows, t.nk == 0);
                 }
@@ -1131,6 +1191,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (et < p.tn && c < p.cols) p.dbp[(size_t)(t.mt * (TM / BM) + rank) * p.ldg + c] = (s_db[0][et] + s_db[1][et]) + (s_db[2][et] + s_db[3][et]);
             }
         }
+        if (MODE == LOGITS && KIND == BF16 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     tc_fence_before();
@@ -1363,7 +1424,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
         L.s_dw = parts_of(t_dw, kb_dw);
         L.slab_dx = L.s_dx > 1 || L.pieces > 1;
         L.slab_dw = L.s_dw > 1;
-        size_t g = (size_t)L.g_planes * np * L.piece, dbp = np / 128 * L.piece;
+        size_t g = (size_t)L.g_planes * np * L.piece, dbp = np / BM * L.piece;
         size_t sdx = L.slab_dx ? (size_t)L.s_dx * np * L.Hp : 0, sdw = L.slab_dw ? (size_t)L.s_dw * up(std::min(o.n_out, L.piece), 128) * L.Hp : 0;
         if (most_of_fewer) {
             // tiles x parts is at most 3/2 kFillCtas (the share of a CTA) more than the tiles, and no part is shorter than least_kb
@@ -1376,7 +1437,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
             const size_t whole = np * (size_t)all, limit = kLossPieceBytes / 2;
             g = std::min((size_t)L.planes * whole, std::max(limit, (size_t)L.planes * np * 2048));
             if (!f32) g = std::max(g, std::min<size_t>(2 * std::min(np, (size_t)256) * all, std::max(limit, 2 * std::min(np, (size_t)256) * 2048)));
-            dbp = std::min(whole, std::max(limit, np * 2048)) / 128;
+            dbp = std::min(whole, std::max(limit, np * 2048)) / BM;
         }
         L.next = take(4 * 2 * (size_t)(most_of_fewer ? cdiv(o.n_out, 2048) : L.pieces));
         L.g = take(2 * g);
@@ -1416,6 +1477,17 @@ static cudaError_t loss_map(CUtensorMap* map, const void* base, uint64_t planes,
 }
 
 typedef void (*LossKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const LossGemm);
+
+// where the tiles of logits store g (its first part): boxes of 16 columns x 32 rows
+static cudaError_t store_map(CUtensorMap* map, void* base, uint64_t rows, uint64_t cols) {
+    cuuint64_t dims[2] = {cols, rows};
+    cuuint64_t strides[1] = {cols * 2};
+    cuuint32_t box[2] = {16, 32};
+    cuuint32_t estr[2] = {1, 1};
+    CUresult r = g_encode_loss(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
 
 template <int MODE, int KIND, bool PAIR>
 static LossKernel loss_kernel_of(bool list) {
@@ -1569,7 +1641,7 @@ cudaError_t loss_run(const LossCall& c) {
     p.bias = c.o.b;
     p.src = r.src; p.target = r.target_c; p.sid = r.sid; p.sq = r.sq;
     const int few = std::min(BM, up(c.N, 8));    // rows of A that a fetch brings
-    CUtensorMap map_x, map_w, map_w64, map_x64, map_g, map_g64;
+    CUtensorMap map_x, map_w, map_w64, map_x64, map_g, map_g64, map_store{};
     if (direct) e = loss_map(&map_x, c.x, 1, c.N, c.o.H, c.N == 1 ? c.o.H : c.ldx, few);
     else e = loss_map(&map_x, r.xc, L.planes, L.Npad, L.Hp, L.Hp, few);
     if (e != cudaSuccess) return e;
@@ -1605,6 +1677,7 @@ cudaError_t loss_run(const LossCall& c) {
     p.dw = c.dw; p.lddw = c.lddw; p.want_dw = c.dw != nullptr; p.dw_vec = vec_rows(c.dw, c.lddw, c.o.H, f32);
     if ((e = loss_map(&map_g, p.g, L.g_planes, L.Npad, L.piece, L.piece, few)) != cudaSuccess) return e;
     if ((e = loss_map(&map_g64, p.g, L.g_planes, L.Npad, L.piece, L.piece, 64)) != cudaSuccess) return e;
+    if ((e = store_map(&map_store, p.g, L.Npad, L.piece)) != cudaSuccess) return e;
     if ((e = loss_map(&map_x64, r.xc, L.planes, L.Npad, L.Hp, L.Hp, 64)) != cudaSuccess) return e;
     if ((e = loss_map(&map_w64, w, L.planes, c.o.n_out, w_cols, ldw, 64)) != cudaSuccess) return e;
     for (int piece = 0; piece < L.pieces; ++piece) {
@@ -1617,7 +1690,7 @@ cudaError_t loss_run(const LossCall& c) {
         const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, L.g_planes, L.pair);
         ring_of(p, l, few, L.tn);
         p.next = r.next + 2 * piece;
-        if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
+        if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_store, map_w, p, c.stream)) != cudaSuccess) return e;
         FinishParams f{};
         f.ctrl = ctrl; f.H = c.o.H; f.Hp = L.Hp; f.cols = p.cols;
         int finish_blocks = 0;
