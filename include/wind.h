@@ -286,7 +286,7 @@ wind_status_t wind_loss_workspace_bytes(const wind_output_t* o, int32_t N, int32
  *   loss, lse  [N] fp32
  *   workspace  device memory, 256-byte aligned, at least wind_loss_workspace_bytes(o, N, 0, 0).  Calls sharing a workspace must not
  *           overlap in time; it carries nothing from one call to the next but the status.
- * N = 0 is a call without rows.  N <= 2^24, n_out < 2^24, H <= 65536, else WIND_ERR_UNSUPPORTED.  A target whose output is masked
+ * N = 0 is a call without rows.  N <= 2^24, n_out < 2^24, N n_out <= 2^40, H <= 65536, else WIND_ERR_UNSUPPORTED.  A target whose output is masked
  * has loss +inf; non-finite rows of x that are not padding have a loss that is NaN or infinite.
  */
 wind_status_t wind_label_loss(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* target, int32_t N, float* loss, float* lse,

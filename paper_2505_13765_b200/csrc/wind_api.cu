@@ -479,7 +479,7 @@ wind_status_t wind_window_first_output(const wind_model_t* m, const void* enc, c
 static wind_status_t check_output(const wind_output_t* o, int N, int K) {
     if (!o || o->n_out < 1 || o->H < 1 || o->ldw < 0 || N < 0 || K < 0) return WIND_ERR_INVALID_ARG;
     if (o->dtype != WIND_DT_F32 && o->dtype != WIND_DT_BF16) return WIND_ERR_INVALID_ARG;
-    if (o->n_out > kLossMaxOut || o->H > kLossMaxH || N > kLossMaxRows || K > kLossMaxK) return WIND_ERR_UNSUPPORTED;
+    if (o->n_out > kLossMaxOut || o->H > kLossMaxH || N > kLossMaxRows || K > kLossMaxK || (long long)N * o->n_out > kLossMaxLogits) return WIND_ERR_UNSUPPORTED;
     return WIND_OK;
 }
 

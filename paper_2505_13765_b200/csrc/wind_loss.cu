@@ -515,45 +515,49 @@ struct __align__(8) Unit {
 };
 
 template <int MODE, int TM>
-__device__ __forceinline__ long long count_units(const LossGemm& p, int n_rows) {
+__device__ __forceinline__ uint32_t count_units(const LossGemm& p, int n_rows) {
     const int mtc = (n_rows + TM - 1) / TM;
-    if (MODE != PRODUCTS) return (long long)mtc * p.n_vt;
-    long long n = 0;
-    if (p.want_dx) n += (long long)p.s_dx * mtc * p.ht;
-    if (p.want_dw) n += (long long)p.s_dw * ((p.cols + TM - 1) / TM) * p.ht;
+    if (MODE != PRODUCTS) return (uint32_t)mtc * p.n_vt;
+    uint32_t n = 0;
+    if (p.want_dx) n += (uint32_t)p.s_dx * mtc * p.ht;
+    if (p.want_dw) n += (uint32_t)p.s_dw * ((p.cols + TM - 1) / TM) * p.ht;
     return n;
 }
 
-// Tiles of TM rows.  Logits: bands of LT_BAND x 128 rows, in a band row tile fastest, so that the CTAs at work share few tiles of x and of W; last tiles of
+// (There are below 2^31 units: the entry points see to that.)  Tiles of TM rows.  Logits: bands of LT_BAND x 128 rows, in a band row tile fastest, so that the CTAs at work share few tiles of x and of W; last tiles of
 // at most half the columns (1024 labels and the blank) come behind all others.  Products: the longer ones first.  CTAs take the next
 // unit when they are through with one, and what is short at the end fills the gaps.
-template <int MODE, int TM, typename Int>
-__device__ __forceinline__ Unit unit_at(const LossGemm& p, int n_rows, Int u) {
+template <int MODE, int TM>
+__device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, uint32_t u, uint32_t n_units) {
     Unit t{};
+    if (u >= n_units) {
+        t.mt = -1;
+        return t;
+    }
     constexpr int BAND = LT_BAND * BM / TM;
     const int mtc = (n_rows + TM - 1) / TM;
     if (MODE != PRODUCTS) {
         const int rest = p.cols - (p.n_vt - 1) * p.tn, wide = p.n_vt - (p.n_vt > 1 && 2 * rest <= p.tn);
         t.nk = p.kb;
-        const Int n_wide = (Int)mtc * wide;
+        const uint32_t n_wide = (uint32_t)mtc * wide;
         if (u >= n_wide) {
             t.nt = wide;
             t.mt = (int)(u - n_wide);
             return t;
         }
-        const Int per_band = (Int)BAND * wide;
+        const uint32_t per_band = (uint32_t)BAND * wide;
         const int band = (int)(u / per_band);
         const int r = (int)(u - band * per_band), in_band = min(BAND, mtc - band * BAND);
         t.nt = in_band == BAND ? r / BAND : r / in_band;
         t.mt = band * BAND + (r - t.nt * in_band);
         return t;
     }
-    const Int n_dx = p.want_dx ? (Int)p.s_dx * mtc * p.ht : 0, n_dw = p.want_dw ? (Int)p.s_dw * ((p.cols + TM - 1) / TM) * p.ht : 0;
+    const uint32_t n_dx = p.want_dx ? (uint32_t)p.s_dx * mtc * p.ht : 0, n_dw = p.want_dw ? (uint32_t)p.s_dw * ((p.cols + TM - 1) / TM) * p.ht : 0;
     t.dw = p.dx_first ? u >= n_dx : u < n_dw;
     if (t.dw == p.dx_first) u -= t.dw ? n_dx : n_dw;
     const int tiles = (t.dw ? (p.cols + TM - 1) / TM : mtc) * p.ht;
     t.part = (int)(u / tiles);
-    const int r = (int)(u - (Int)t.part * tiles);
+    const int r = (int)(u - (uint32_t)t.part * tiles);
     t.mt = r / p.ht;
     t.nt = r - t.mt * p.ht;
     const int kb = ((t.dw ? n_rows : p.cols) + BK - 1) / BK, s = t.dw ? p.s_dw : p.s_dx;
@@ -565,17 +569,6 @@ __device__ __forceinline__ Unit unit_at(const LossGemm& p, int n_rows, Int u) {
     }
     return t;
 }
-// (divisions of 64 bits take a thousand cycles, which at the start of a kernel nothing hides)
-template <int MODE, int TM>
-__device__ __forceinline__ Unit unit_of(const LossGemm& p, int n_rows, long long u, long long n_units) {
-    if (u < 0 || u >= n_units) {
-        Unit none{};
-        none.mt = -1;
-        return none;
-    }
-    return n_units < 0x7fffffff ? unit_at<MODE, TM, uint32_t>(p, n_rows, (uint32_t)u) : unit_at<MODE, TM, long long>(p, n_rows, u);
-}
-
 // A CTA's first unit is that of its number; the others are handed on through a ring, by the one thread that fetches operands and
 // takes them, to the one that issues the products and to the epilogue.  They go as tiles, worked out while earlier operands are under
 // way: left to the issuing thread, that stood 1200 cycles between one tile's products and the next one's.
@@ -965,7 +958,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const uint32_t tmem_base = tmem_slot;
     wait_for_previous();
     const int n_rows = MODE == FORWARD && p.direct ? p.direct : p.ctrl->n_rows;
-    const long long n_units = count_units<MODE, TM>(p, n_rows);
+    const uint32_t n_units = count_units<MODE, TM>(p, n_rows);
     // a short kernel lets the next one start at once; blocks that wait beside a long one slow it (two per cent of a text model's step)
     if (n_units <= ctas) let_next_start();
 
@@ -979,16 +972,16 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             bool ok = true;
             Unit t = first;
             for (uint32_t n = 0; t.mt >= 0; ++n) {
-                const int taken = PAIR && rank ? 0 : p.next ? atomicAdd(p.next, 1) : (int)(n * ctas + cta);   // (there when this unit's first K blocks are under way)
+                const uint32_t taken = PAIR && rank ? 0 : p.next ? (uint32_t)atomicAdd(p.next, 1) : n * ctas + cta;   // (there when this unit's first K blocks are under way)
                 // The next unit is handed on once the ring is full of this one: at that point nothing waits for this unit's epilogue, which
-                // waits for the answer (and empties fp32's accumulators, without which the rest could not be fetched).
+                // waits for the answer.
                 Unit then{};
                 auto hand_on = [&] {
                     if (PAIR && rank) {
                         then = next_unit<PAIR>(units, n, rank, &abort_flag);
                         return then.mt >= 0 || !abort_flag;
                     }
-                    then = unit_of<MODE, TM>(p, n_rows, (long long)ctas + taken, n_units);
+                    then = unit_of<MODE, TM>(p, n_rows, ctas + taken, n_units);
                     return give_unit<PAIR>(units, n, then, &abort_flag);
                 };
                 // (a pair: half the columns each, 32 at least)
@@ -996,7 +989,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const int panels = PAIR ? (half + 63) / 64 : (unit_cols<MODE>(p, t) + 63) / 64;
                 const int a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2;
                 const uint32_t bytes = A_PARTS * a_part + B_PARTS * (MODE == PRODUCTS ? panels * PANEL_BYTES : p.b_bytes);
-                const int hand_at = PAIR && rank ? -1 : t.k0 + min(t.nk, p.stages) - 1;   // (the pair's other CTA hears of it when it is through)
+                const int hand_at = KIND == F32 || (PAIR && rank) ? -1 : t.k0 + min(t.nk, p.stages) - 1;   // (fp32, and a pair's other CTA: when it is through)
                 for (int kb = t.k0; kb < t.k0 + t.nk; ++kb) {
                     if (!mbar_wait(&empty_bar[s], (turn & 1) ^ 1, &abort_flag)) { ok = false; break; }
                     uint8_t* b = a + A_PARTS * a_part;
@@ -1023,7 +1016,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     if (++s == p.stages) { s = 0; ++turn; a = smem; }
                     if (kb == hand_at && !hand_on()) { ok = false; break; }
                 }
-                if (ok && (t.nk == 0 || (PAIR && rank))) ok = hand_on();
+                if (ok && (t.nk == 0 || hand_at < 0)) ok = hand_on();
                 if (!ok) break;
                 t = then;
             }
@@ -1116,10 +1109,18 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             // One thread asks for the next unit, which is there before this one's accumulator is; all warps hear the same answer, so that
             // they leave together.  (A warp whose wait runs out goes on without waiting: the others still meet it at the barriers.)
-            if (et == 0) write_unit(&s_unit[n_tile & 1], next_unit<PAIR>(units, n_tile, rank, &abort_flag));
-            __syncwarp();
-            asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
-            then = read_unit(&s_unit[n_tile & 1]);
+            // fp32 asks when it is through with this one: its operands are not all fetched before that, its accumulators being emptied here.
+            auto ask = [&] {
+                if (et == 0) write_unit(&s_unit[n_tile & 1], next_unit<PAIR>(units, n_tile, rank, &abort_flag));
+                __syncwarp();
+                asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
+                then = read_unit(&s_unit[n_tile & 1]);
+            };
+            if (KIND != F32) ask();
+            else if (MODE != PRODUCTS) {
+                __syncwarp();
+                asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
+            }
             // fp32: an accumulator takes one K block, whose sum is added up here.  (Tensor cores cut where they add; over a long K that
             // is an error of 2^-25 an addition, all one way: 5e-6 of dW over 20 000 rows.)
             float sums[KIND == F32 ? S::CHUNKS * 32 : 1];
@@ -1190,6 +1191,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const int c = t.nt * p.tn + et;
                 if (et < p.tn && c < p.cols) p.dbp[(size_t)(t.mt * (TM / BM) + rank) * p.ldg + c] = (s_db[0][et] + s_db[1][et]) + (s_db[2][et] + s_db[3][et]);
             }
+            if (KIND == F32) ask();
         }
         if (MODE == LOGITS && KIND == BF16 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }

@@ -10,6 +10,7 @@ namespace wind {
 
 constexpr int kLossMaxK = 256;            // teacher's entries of a row
 constexpr int kLossMaxCtas = 256;
+constexpr long long kLossMaxLogits = 1ll << 40;   // N n_out
 constexpr int kLossMaxRows = 1 << 24;
 constexpr int kLossMaxOut = (1 << 24) - 1;
 constexpr int kLossMaxH = 1 << 16;

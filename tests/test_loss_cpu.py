@@ -34,7 +34,7 @@ def test_workspace_sizes(lib):
         assert size(lib, layer(**bad), 1) == -bd.WIND_ERR_INVALID_ARG, bad
     assert size(lib, layer(), -1) == -bd.WIND_ERR_INVALID_ARG
     assert size(lib, layer(), 1, -1) == -bd.WIND_ERR_INVALID_ARG
-    for N, K, kw in ((1, 257, {}), ((1 << 24) + 1, 0, {}), (1, 0, dict(n_out=1 << 24)), (1, 0, dict(H=65537))):
+    for N, K, kw in ((1, 257, {}), ((1 << 24) + 1, 0, {}), (1, 0, dict(n_out=1 << 24)), (1 << 24, 0, dict(n_out=1 << 17)), (1, 0, dict(H=65537))):
         assert size(lib, layer(**kw), N, K) == -bd.WIND_ERR_UNSUPPORTED
     assert size(lib, layer(), 0) > 0
     # a loss keeps three numbers per row and 128 outputs, never a row's logits
