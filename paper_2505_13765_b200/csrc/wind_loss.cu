@@ -353,14 +353,34 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
     __syncthreads();
     const size_t plane = (size_t)p.Npad * p.Hp;
     const size_t es = F32 ? 4 : 2;
-    // eight columns a thread, over all rows of the block: their loads are under way together
+    // eight columns a thread, over all rows of the block; four loads of a thread are under way together
     const int per_row = p.Hp / 8, chunks = here * per_row;
-#pragma unroll 4
-    for (int i = me; i < chunks; i += 256) {
-        const int k = i / per_row, c = (i - k * per_row) * 8;
-        float v[8];
-        load8<F32>(static_cast<const uint8_t*>(p.x) + (size_t)(r0 + s_row[k]) * p.ldx * es, c, p.H, p.x_vec, v);
-        store8<F32>(p.xc + (size_t)(first_pos + k) * p.Hp + c, plane, v);
+    if (!F32 && p.x_vec) {
+        const uint4* x = static_cast<const uint4*>(p.x);
+        uint4* out = reinterpret_cast<uint4*>(p.xc);
+        const int64_t ld = p.ldx / 8;
+        const int in_row = p.H / 8;
+        for (int i0 = me; i0 < chunks; i0 += 4 * 256) {
+            uint4 v[4];
+            int to[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int i = i0 + q * 256, k = i / per_row, c = i - k * per_row;
+                to[q] = k * per_row + c;
+                v[q] = i < chunks && c < in_row ? x[(size_t)(r0 + s_row[k]) * ld + c] : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (i0 + q * 256 < chunks) out[(size_t)first_pos * per_row + to[q]] = v[q];
+        }
+    } else {
+#pragma unroll 2
+        for (int i = me; i < chunks; i += 256) {
+            const int k = i / per_row, c = (i - k * per_row) * 8;
+            float v[8];
+            load8<F32>(static_cast<const uint8_t*>(p.x) + (size_t)(r0 + s_row[k]) * p.ldx * es, c, p.H, p.x_vec, v);
+            store8<F32>(p.xc + (size_t)(first_pos + k) * p.Hp + c, plane, v);
+        }
     }
     if (me < here) {
         const int r = r0 + s_row[me], j = first_pos + me;
@@ -402,8 +422,7 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
         const float zero[8] = {};
         if (p.dw)
             for (int j = total + warp; j < (total + 63) / 64 * 64; j += 8)
-               
-            for (int c = lane * 8; c < p.Hp; c += 256) store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, zero);
+                for (int c = lane * 8; c < p.Hp; c += 256) store8<F32>(p.xc + (size_t)j * p.Hp + c, plane, zero);
         if (p.db && total == 0)      // (no tile of logits is there to write it)
             for (int v = threadIdx.x; v < p.n_out; v += 256) p.db[v] = 0.f;
     }
@@ -430,7 +449,8 @@ struct LossGemm {
     float rtau;                   // 1 / tau
     const float* bias;
     const int32_t* src; const int32_t* target; const int32_t* sid; const float* sq;
-    float *pm, *ps, *pq;          // FORWARD: [parts][Npad]
+    float *pm, *ps, *pq;          // FORWARD: [parts][Npad]; where a row has one part its results instead:
+    float *loss, *lse; const float* ent; float tau;
     const float* scale; const float* nlse;
     __nv_bfloat16* g; int ldg; size_t g_plane; float* dbp;   // LOGITS
     // PRODUCTS
@@ -734,6 +754,13 @@ __device__ __forceinline__ void join(RowPart& a, float m, float s, float qz) {
     a.s = a.s * exp2_fast((a.m - base) * kLog2e) + s * exp2_fast((m - base) * kLog2e);
     a.m = m1;
     a.qz += qz;
+}
+
+// A row's loss and log-sum-exp.  (Maximum minus the targets' mean logit first: both are large where the logits are.)
+__device__ __forceinline__ void row_result(const RowPart& a, int r, const float* ent, float tau, float* loss, float* lse) {
+    const float log_s = logf(a.s), ce = (a.m - a.qz) + log_s;
+    loss[r] = ent ? tau * tau * (ent[r] + ce) : ce;
+    lse[r] = a.m + log_s;
 }
 
 // FORWARD epilogue of one row's columns (n_cols of them are outputs) from `col` on.
@@ -1179,10 +1206,14 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (group == 0 && there) {
 #pragma unroll
                     for (int i = 1; i < S::GROUPS; ++i) join(part, s_part[i][0][row_in_tile], s_part[i][1][row_in_tile], s_part[i][2][row_in_tile]);
-                    const size_t at = (size_t)t.nt * p.Npad + row;
-                    p.pm[at] = part.m;
-                    p.ps[at] = part.s;
-                    p.pq[at] = part.qz;
+                    if (p.loss) {
+                        row_result(part, p.src[row], p.ent, p.tau, p.loss, p.lse);
+                    } else {
+                        const size_t at = (size_t)t.nt * p.Npad + row;
+                        p.pm[at] = part.m;
+                        p.ps[at] = part.s;
+                        p.pq[at] = part.qz;
+                    }
                 }
             }
             if (MODE == LOGITS && p.dbp) {
@@ -1269,11 +1300,11 @@ __global__ void __launch_bounds__(256) loss_combine_kernel(const CombineParams p
     if (threadIdx.x >= 8 || j >= n) return;
     const int r = p.direct ? j : p.src[j];
     const uint8_t mark = p.direct ? mark_of(p.target, p.mark, p.n_out, r) : (uint8_t)ROW_COUNTS;
-    const float log_s = logf(s);
-    // (maximum minus the targets' mean logit first: both are large where the logits are)
-    const float ce = (m - qz) + log_s, none = mark == ROW_BAD ? CUDART_NAN_F : 0.f;
-    p.loss[r] = mark != ROW_COUNTS ? none : p.ent ? p.tau * p.tau * (p.ent[r] + ce) : ce;
-    p.lse[r] = mark != ROW_COUNTS ? none : m + log_s;
+    if (mark == ROW_COUNTS) {
+        row_result(RowPart{m, s, qz}, r, p.ent, p.tau, p.loss, p.lse);
+    } else {
+        p.loss[r] = p.lse[r] = mark == ROW_BAD ? CUDART_NAN_F : 0.f;
+    }
 }
 
 // What is left of a piece: partial sums of dW and, behind the last piece, of dx to their places, and db from the row tiles' column sums.
@@ -1659,7 +1690,10 @@ cudaError_t loss_run(const LossCall& c) {
         ring_of(p, l, few, L.tn);
         p.next = direct ? nullptr : r.next;
         if (direct) { p.direct = c.N; p.src = nullptr; p.target = c.target; }
+        const bool final = !direct && L.parts == 1;     // (no launch for joining what is one part)
+        if (final) { p.loss = c.loss; p.lse = c.lse_out; p.ent = c.K ? r.ent : nullptr; p.tau = c.tau; }
         if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
+        if (final) return cudaSuccess;
         CombineParams q{};
         q.ctrl = ctrl; q.src = r.src; q.pm = p.pm; q.ps = p.ps; q.pq = p.pq; q.parts = L.parts; q.Npad = L.Npad;
         q.ent = c.K ? r.ent : nullptr; q.tau = c.tau; q.loss = c.loss; q.lse = c.lse_out;
