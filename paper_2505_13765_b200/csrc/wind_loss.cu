@@ -880,8 +880,10 @@ __device__ __forceinline__ void logits_row(const LossGemm& p, const CUtensorMap*
 }
 
 // PRODUCTS epilogue of one row's columns from h0 on; zero: the sum has no term.
+// Rows that start anywhere go through the warp's 2 KB of shared memory, 16 columns at a time, and leave two rows an instruction: single
+// values straight from registers, 32 rows an instruction, made 0.9 ms of a dW of 52104 x 1429 bf16.
 template <int KIND, int CHUNKS>
-__device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, uint32_t taddr, const float* sums, int h0, int row, int n_rows,
+__device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, float* stage, uint32_t taddr, const float* sums, int h0, int row, int n_rows,
                                             bool zero) {
     constexpr bool f32 = KIND == F32;
     const bool there = row < (t.dw ? p.cols : n_rows);             // row, of dx: a gathered row; of dW: an output of the piece
@@ -905,7 +907,24 @@ __device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, ui
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
         } else fetch32<KIND>(v, taddr, sums, c);
-        if (!there) {
+        if (!slab && !(vec && h + 32 <= h1)) {
+            const int lane = threadIdx.x & 31;
+            const unsigned long long mine = reinterpret_cast<unsigned long long>(out);
+#pragma unroll
+            for (int i0 = 0; i0 < 32; i0 += 16) {
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) stage[lane * 16 + (i ^ (lane & 15))] = v[i0 + i];
+                __syncwarp();
+                const int col = h + i0 + (lane & 15);
+#pragma unroll 4
+                for (int r = lane >> 4; r < 32; r += 2) {
+                    uint8_t* to = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, mine, r));
+                    const float x = stage[r * 16 + ((lane & 15) ^ (r & 15))];
+                    if (to && col < h1) store_one<f32>(to, col, x);
+                }
+            }
+        } else if (!there) {
         } else if (sum) {
             if (!t.dw && p.add_dx) {
                 const float4* d = reinterpret_cast<const float4*>(sum + h);
@@ -917,7 +936,7 @@ __device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, ui
             }
 #pragma unroll
             for (int i = 0; i < 32; i += 8) store_sector(sum + h + i, reinterpret_cast<const uint32_t*>(v + i));
-        } else if (vec == 2 && h + 32 <= h1) {
+        } else if (vec == 2) {
             if constexpr (f32) {
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) store_sector(reinterpret_cast<float*>(out) + h + i, reinterpret_cast<const uint32_t*>(v + i));
@@ -925,7 +944,7 @@ __device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, ui
 #pragma unroll
                 for (int i = 0; i < 32; i += 16) store16<1>(reinterpret_cast<__nv_bfloat16*>(out) + h + i, 0, v + i);
             }
-        } else if (vec && h + 32 <= h1) {
+        } else {
             if constexpr (f32) {
                 float4* d = reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + h);
 #pragma unroll
@@ -934,10 +953,6 @@ __device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, ui
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) store8<false>(reinterpret_cast<__nv_bfloat16*>(out) + h + i, 0, v + i);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (h + i < h1) store_one<f32>(out, h + i, v[i]);
         }
     }
 }
@@ -1118,7 +1133,8 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const int my0 = group * width;                     // first column of this warp's, in the tile
         uint32_t n_acc = 0, n_tile = 0;
         bool ok = true;
-        uint8_t* stage = smem + (kRingBytes - A_STAGE_BYTES) + (warp - 2) * 1024;   // (LOGITS of bf16: its A is never short)
+        // behind the ring, where a short A is read to no purpose: 16 KB for the epilogue's warps
+        uint8_t* stage = smem + (kRingBytes - A_STAGE_BYTES) + (warp - 2) * (32 * A_STAGE_BYTES / EPI);
         Unit then = first;
         for (; then.mt >= 0; ++n_tile) {
             const Unit t = then;
@@ -1186,7 +1202,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     logits_row<LIST, KIND, S::CHUNKS>(p, &map_a2, stage, taddr, sums, bias + my0, t.nt * p.tn + my0, width, row, there, scale, nlse, targets,
                                                       &s_db[q][my0]);
                 } else {
-                    product_row<KIND, S::CHUNKS>(p, t, taddr, sums, t.nt * p.tn + my0, row, n_rows, t.nk == 0);
+                    product_row<KIND, S::CHUNKS>(p, t, reinterpret_cast<float*>(stage), taddr, sums, t.nt * p.tn + my0, row, n_rows, t.nk == 0);
                 }
             }
             if (KIND != F32 && t.nk > 0) {
