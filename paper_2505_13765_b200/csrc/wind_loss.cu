@@ -71,7 +71,7 @@ struct RowsParams {
     float tau;
     const int32_t* target; const int32_t* ids; const float* y;
     const void* x; int64_t ldx;
-    int32_t* counts; uint8_t* mark; int32_t* src; int32_t* target_c; float* scale_c; float* nlse_c; int32_t* sid; float* sq; float* ent;
+    int32_t* counts; uint8_t* mark; int32_t* src; int32_t* target_c; float* scale_c; float* nlse_c; int2* list; uint8_t* where; int where_ld; float* ent;
     __nv_bfloat16* xc;
     float* loss; float* lse_out;
     const float* lse; const float* dloss;
@@ -86,13 +86,15 @@ __device__ __forceinline__ uint8_t mark_of(const int32_t* target, const uint8_t*
 
 __device__ __forceinline__ uint8_t row_mark(const RowsParams& p, int r) { return mark_of(p.target, p.K ? p.mark : nullptr, p.n_out, r); }
 
+constexpr int WHERE_WORDS = 512;
 constexpr uint32_t NO_LABEL = 0xffffffu;   // (n_out is below 2^24)
 
 // The teacher's list of a row, a warp each: probabilities over the entries that are there, and the entries by rising label (equal
 // labels in their order), so that the epilogues walk a list along their columns.  The place of an entry is the number of keys
-// label * 256 + entry below its own: K^2 / 32 comparisons a lane.
+// label * 256 + entry below its own: K^2 / 32 comparisons a lane.  `where` has for every 32nd output the number of entries below it (255
+// for 256), a byte each: the epilogues start there (searching, 16 warps a tile, cost them 4000 cycles a tile).
 __global__ void __launch_bounds__(256) loss_list_kernel(const RowsParams p) {
-    __shared__ __align__(16) uint32_t s_keys[8][kLossMaxK];
+    __shared__ __align__(16) uint32_t s_keys[8][kLossMaxK], s_where[8][WHERE_WORDS];
     let_next_start();
     wait_for_previous();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -143,8 +145,36 @@ __global__ void __launch_bounds__(256) loss_list_kernel(const RowsParams p) {
             const uint4 o = *reinterpret_cast<const uint4*>(keys + j);
             place += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
         }
-        p.sid[(size_t)r * p.K + place] = key >> 8 == NO_LABEL ? 0x7fffffff : (int)(key >> 8);
-        p.sq[(size_t)r * p.K + place] = q;
+        const int label = key >> 8 == NO_LABEL ? 0x7fffffff : (int)(key >> 8);
+        p.list[(size_t)r * p.K + place] = make_int2(label, __float_as_int(q));
+        if (place == 255) keys[k] = 0xffffffffu;       // (never the reason to start behind entry 255)
+    }
+    // `where`: how many labels lie in each 32 outputs, a byte each, and their running sums
+    uint32_t* w = s_where[warp];
+    uint32_t below = 0;
+    for (int b0 = 0; b0 < p.where_ld; b0 += 4 * WHERE_WORDS) {
+        const int words = min(WHERE_WORDS, (p.where_ld - b0) / 4);
+        __syncwarp();
+        for (int i = lane; i < words; i += 32) w[i] = 0;
+        __syncwarp();
+        for (int k = lane; k < p.K; k += 32) {
+            const uint32_t key = keys[k];
+            const int at = (int)(key >> 13) + 1 - b0;      // label / 32 + 1
+            if (key >> 8 != NO_LABEL && at >= 0 && at < 4 * words) atomicAdd(&w[at >> 2], 1u << (8 * (at & 3)));
+        }
+        __syncwarp();
+        for (int i0 = 0; i0 < words; i0 += 32) {
+            uint32_t sums = i0 + lane < words ? w[i0 + lane] * 0x01010101u : 0u;      // running sums of the word's bytes
+            uint32_t upto = sums >> 24;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            sums += (below + upto - (sums >> 24)) * 0x01010101u;
+            if (i0 + lane < words) reinterpret_cast<uint32_t*>(p.where + (size_t)r * p.where_ld + b0)[i0 + lane] = sums;
+            below += __shfl_sync(0xffffffffu, upto, 31);
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ent += __shfl_xor_sync(0xffffffffu, ent, o);
@@ -448,7 +478,7 @@ struct LossGemm {
     int direct;                   // FORWARD: x as the caller has it, this many rows; 0: gathered rows
     float rtau;                   // 1 / tau
     const float* bias;
-    const int32_t* src; const int32_t* target; const int32_t* sid; const float* sq;
+    const int32_t* src; const int32_t* target; const int2* list; const uint8_t* where; int where_ld;
     float *pm, *ps, *pq;          // FORWARD: [parts][Npad]; where a row has one part its results instead:
     float *loss, *lse; const float* ent; float tau;
     const float* scale; const float* nlse;
@@ -712,25 +742,37 @@ __device__ __forceinline__ void fetch32(float* v, uint32_t taddr, const float* s
     }
 }
 
-// A row's target distribution, met along its columns.
+// A row's target distribution, met along its columns (from `col` on, a multiple of 32).  The next two entries of a list are on hand:
+// fetching one where it is met took the warp 700 cycles.
 template <bool LIST>
 struct Targets {
-    int next = 0x7fffffff, cur = 0, K;
-    const int32_t* sid = nullptr;
-    const float* sq = nullptr;
+    int next = 0x7fffffff, after = 0x7fffffff, cur = 0, K;
+    float q = 1.f, q_after = 0.f;
+    const int2* list = nullptr;
     __device__ __forceinline__ Targets(const LossGemm& p, int row, bool there, int col) : K(p.K) {
         if (!there) return;
         if (!LIST) { next = p.target[row]; return; }
-        const size_t at = (size_t)(p.src ? p.src[row] : row) * K;
-        sid = p.sid + at;
-        sq = p.sq + at;
-        int lo = 0, hi = K;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (sid[mid] < col) lo = mid + 1; else hi = mid;
+        const size_t r = p.src ? p.src[row] : row;
+        list = p.list + r * K;
+        cur = p.where[r * p.where_ld + (col >> 5)];
+        if (cur < K) {
+            const int2 a = list[cur];
+            next = a.x; q = __int_as_float(a.y);
         }
-        cur = lo;
-        if (cur < K) next = sid[cur];
+        fetch_after();
+        if (next < col) step();          // (K = 256: `where` says 255 for none)
+    }
+    __device__ __forceinline__ void fetch_after() {
+        after = 0x7fffffff;
+        if (cur + 1 < K) {
+            const int2 a = list[cur + 1];
+            after = a.x; q_after = __int_as_float(a.y);
+        }
+    }
+    __device__ __forceinline__ void step() {
+        next = after; q = q_after;
+        ++cur;
+        fetch_after();
     }
     // f(column, weight) for the targets in [col, col + 32)
     template <typename F>
@@ -739,9 +781,8 @@ struct Targets {
             if (next >= col && next < col + 32) f(next - col, 1.f);
         } else {
             while (next < col + 32) {
-                f(next - col, sq[cur]);
-                ++cur;
-                next = cur < K ? sid[cur] : 0x7fffffff;
+                f(next - col, q);
+                step();
             }
         }
     }
@@ -1431,8 +1472,9 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
     L.target = take(K ? 0 : 4 * np);
     L.scale = take(grad ? 4 * np : 0);
     L.nlse = take(grad ? 4 * np : 0);
-    L.sid = take(4 * (size_t)N * K);
-    L.sq = take(4 * (size_t)N * K);
+    L.where_ld = up(cdiv(o.n_out, 32), 4);
+    L.list = take(8 * (size_t)N * K);
+    L.where = take(K ? (size_t)N * L.where_ld : 0);
     L.ent = take(K ? 4 * np : 0);
     L.x = take(2 * (size_t)L.planes * np * L.Hp);
     L.w = take(L.pack_w ? 2 * (size_t)L.planes * o.n_out * L.Hp : 0);
@@ -1649,8 +1691,9 @@ cudaError_t loss_run(const LossCall& c) {
     r.target_c = reinterpret_cast<int32_t*>(c.ws + L.target);
     r.scale_c = reinterpret_cast<float*>(c.ws + L.scale);
     r.nlse_c = reinterpret_cast<float*>(c.ws + L.nlse);
-    r.sid = reinterpret_cast<int32_t*>(c.ws + L.sid);
-    r.sq = reinterpret_cast<float*>(c.ws + L.sq);
+    r.list = reinterpret_cast<int2*>(c.ws + L.list);
+    r.where = c.ws + L.where;
+    r.where_ld = L.where_ld;
     r.ent = reinterpret_cast<float*>(c.ws + L.ent);
     r.xc = reinterpret_cast<__nv_bfloat16*>(c.ws + L.x);
     r.loss = c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.dloss; r.dx = c.dx; r.lddx = c.lddx;
@@ -1688,7 +1731,7 @@ cudaError_t loss_run(const LossCall& c) {
     p.tn = L.tn;
     p.rtau = 1.f / c.tau;
     p.bias = c.o.b;
-    p.src = r.src; p.target = r.target_c; p.sid = r.sid; p.sq = r.sq;
+    p.src = r.src; p.target = r.target_c; p.list = r.list; p.where = r.where; p.where_ld = r.where_ld;
     const int few = std::min(BM, up(c.N, 8));    // rows of A that a fetch brings
     CUtensorMap map_x, map_w, map_w64, map_x64, map_g, map_g64, map_store{};
     if (direct) e = loss_map(&map_x, c.x, 1, c.N, c.o.H, c.N == 1 ? c.o.H : c.ldx, few);

@@ -28,6 +28,7 @@ struct LossLayout {
     int planes;        // bf16 parts of an operand: 1 (bf16) or 3 (fp32)
     int g_planes;      // of the gradient's share of logits: 1, 2 (bf16, few rows) or 3 (fp32)
     int pack_w;        // W is laid out again: fp32, or rows that TMA cannot start on
+    int where_ld;      // bytes of a row's index into its list of the teacher's entries
     int Hp, Npad;      // H up to a multiple of 64, N up to a multiple of 128
     int piece;         // outputs of a piece (gradient), a multiple of 256
     int pieces;
@@ -36,7 +37,7 @@ struct LossLayout {
     int pair, pair_products;   // whether two CTAs make a tile, of logits and of dx and dW
     int s_dx, s_dw;    // parts that the sums of dx (over a piece's outputs) and dW (over the rows) are cut into
     int slab_dx, slab_dw;   // whether dx / dW go through fp32 partial sums
-    size_t ctrl, next, counts, mark, src, target, scale, nlse, sid, sq, ent, x, w, pm, ps, pq, g, dbp, sdx, sdw, total;
+    size_t ctrl, next, counts, mark, src, target, scale, nlse, list, where, ent, x, w, pm, ps, pq, g, dbp, sdx, sdw, total;
 };
 
 struct LossCall {
