@@ -44,7 +44,7 @@ namespace wind {
 // ---------------------------------------------------------------------------
 // sizes
 // ---------------------------------------------------------------------------
-constexpr int LT_BAND = 16;               // row tiles that are worked on together (see tile_of)
+constexpr int LT_BAND = 16;               // row tiles that are worked on together (see unit_of)
 constexpr int ROWS_COUNTED = 32768;       // longer calls have the rows that count counted by a kernel of its own, so many at a time
 constexpr int PANEL_BYTES = 64 * BK * 2;  // 64 x 64 bf16
 constexpr int kFillCtas = 148;            // CTAs that a product is cut for
@@ -299,8 +299,8 @@ __device__ __forceinline__ void pack_w(const RowsParams& p, int block, int block
     }
 }
 
-// A block takes per_block rows.  Where its first row that counts goes is the number of such rows before it,
-// which every block finds out for itself: reading up to ROWS_COUNTED marks from L2 is quicker than another launch.
+// A block takes per_block rows.  Where its first row that counts goes is the number of such rows before it, which every block finds out
+// for itself: reading up to ROWS_COUNTED marks from L2 is quicker than another launch.
 template <bool F32>
 __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
     __shared__ int s_before[8];
@@ -498,7 +498,6 @@ struct Shape {
     static constexpr int TN = KIND == F32 ? 128 : 256;                                       // most columns of a tile (BM = 128 rows)
     static constexpr int A_PARTS = KIND == F32 ? 3 : (KIND == BF16_FINE && MODE == PRODUCTS ? 2 : 1), B_PARTS = KIND == F32 ? 3 : 1;
     static constexpr int TERMS = KIND == F32 ? 6 : A_PARTS;
-    static constexpr int WORST = A_PARTS * A_STAGE_BYTES + B_PARTS * TN * BK * 2;            // bytes of a full stage
     // Groups of four epilogue warps (one per tensor-memory lane quadrant), each with its columns of a tile.  A row of logits is a chain
     // of maxima, exponentials and sums: 16 warps hide more of it than 8 (which is what fp32's sums leave registers for).
     static constexpr int GROUPS = MODE != PRODUCTS && KIND != F32 ? 4 : 2;

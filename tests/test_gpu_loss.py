@@ -115,7 +115,22 @@ def reference(c, grad=True):
     out["tol_dx"] = (g_off + (sum_x + cut) * g.abs()) @ w.abs() * (1 + 2.0 ** -7) + last * out["dx"].abs()
     out["tol_dw"] = (g_off + (sum_w + cut) * g.abs()).T @ x.abs() * (1 + 2.0 ** -7) + last * out["dw"].abs()
     out["tol_db"] = (off + (N / 32 + 16) * 2.0 ** -23 * g.abs()).sum(0)
+    out["abs_dw"], out["abs_db"] = g.abs().T @ x.abs(), g.abs().sum(0)
     return out
+
+
+def verify_in_slices(got, c, slice_rows):
+    """verify() for more rows than a reference of 64 bits has room for; sums over all rows have that many more fp32 steps than a slice's."""
+    N, total = c["x"].shape[0], {}
+    for r0 in range(0, N, slice_rows):
+        rows = slice(r0, min(N, r0 + slice_rows))
+        want = reference({k: (v[rows] if k in ("x", "t", "ids", "y", "dloss") else v) for k, v in c.items()})
+        verify({k: got[k][rows] for k in ("loss", "lse", "dx")}, want, r0)
+        for k in ("dw", "db", "tol_dw", "tol_db", "abs_dw", "abs_db"):
+            total[k] = total.get(k, 0) + want[k]
+    steps = N / 16 * (6 if c["w"].dtype == torch.float32 else 1) * 2.0 ** -23
+    for k in ("dw", "db"):
+        assert bool(((got[k].double() - total[k]).abs() <= total["tol_" + k] + steps * total["abs_" + k]).all()), k
 
 
 def call(pkg, c, ws=None, grad=True, dx=None, dw=None, want=("dx", "dw", "db"), stream=None, check=True):
@@ -267,6 +282,76 @@ def test_masked_outputs(pkg, dtype):
     assert bool(torch.isfinite(got["loss"][6:]).all())
 
 
+@pytest.mark.parametrize("N", [70, 400])
+def test_full_lists_of_low_labels(pkg, N):
+    """256 entries that all lie in the first few outputs (and some lists that end at an output's group of 32), no entry behind."""
+    c = make(23, "bf16", N, 64, 700, 256, pad=0.0, full=True)
+    c["ids"] = (c["ids"] % 20).contiguous()
+    c["ids"][3] = 31
+    c["ids"][4] = 32
+    c["ids"][5] = 699
+    c["ids"][6, :128], c["ids"][6, 128:] = 255, 256
+    verify(call(pkg, c), reference(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [0, 5])
+def test_vectors_that_start_anywhere(pkg, dtype, K):
+    """Everything but the matrices at addresses that are multiples of 4 bytes alone."""
+    for N in (60, 700):
+        c = make(24, dtype, N, 72, 333, K, pad=0.2)
+        ref = reference(c)
+
+        def shifted(t):
+            buf = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+            v = buf[1:].view(t.shape)
+            v.copy_(t)
+            return v
+
+        for k in ("t", "ids", "y", "dloss", "b"):
+            if k in c:
+                c[k] = shifted(c[k])
+        ws = pkg.alloc_loss_workspace(c["w"], N, K, True)
+        loss, lse, db = (shifted(torch.full((n,), math.nan, device=DEV)) for n in (N, N, 333))
+        dx, dw = torch.empty(N, 72, dtype=DT[dtype], device=DEV), torch.empty(333, 72, dtype=DT[dtype], device=DEV)
+        rows = (c["ids"], c["y"], c["tau"]) if K else (c["t"],)
+        fwd, bwd = (pkg.wind_distill_loss, pkg.wind_distill_loss_grad) if K else (pkg.wind_label_loss, pkg.wind_label_loss_grad)
+        fwd(c["x"], c["w"], c["b"], *rows, loss, lse, ws, check=True)
+        bwd(c["x"], c["w"], c["b"], *rows, lse, c["dloss"], dx, dw, db, ws, check=True)
+        verify(dict(loss=loss, lse=lse, dx=dx, dw=dw, db=db), ref)
+
+
+def test_rows_far_apart(pkg):
+    """Offsets that pass 32 bits: rows of x, W, dx and dW more than 2^31 bytes, then more than 2^31 elements, from the first."""
+    ld = 1_100_000_000
+    c = make(25, "bf16", 3, 64, 3, pad=0.0)
+    ref = reference(c)
+    out = {}
+    for k in ("x", "w", "dx", "dw"):
+        buf = torch.empty(2 * ld + 64, dtype=torch.bfloat16, device=DEV)
+        out[k] = buf.as_strided((3, 64), (ld, 1))
+    for k in ("x", "w"):
+        out[k].copy_(c[k])
+        c[k] = out[k]
+    verify(call(pkg, c, dx=out["dx"], dw=out["dw"]), ref)
+
+
+def test_many_rows(pkg):
+    """More than 2^31 values of g in one piece, and lists of more rows than a block counts."""
+    for N, H, V, K in ((1_060_000, 8, 2100, 0), (70_001, 16, 70, 3)):
+        c = make(26, "bf16", N, H, V, K, pad=0.1)
+        verify_in_slices(call(pkg, c), c, 50_000)
+
+
+def test_a_workspace_of_more_rows_serves_fewer(pkg):
+    for dtype, K in (("bf16", 0), ("bf16", 6), ("f32", 0)):
+        c = make(27, dtype, 3000, 136, 700, K)
+        ws = pkg.alloc_loss_workspace(c["w"], 3000, K, True)
+        for n in (3000, 1, 129, 2049, 300):
+            d = {k: (v[:n] if k in ("x", "t", "ids", "y", "dloss") else v) for k, v in c.items()}
+            verify(call(pkg, d, ws=ws), reference(d), n)
+
+
 def test_without_bias_and_without_weights(pkg):
     c = make(31, "bf16", 100, 64, 300, bias=False)
     c["dloss"] = None
@@ -286,20 +371,7 @@ def test_several_pieces_of_the_outputs(pkg, dtype, N, H, V):
     c = make(41, dtype, N, H, V, pad=0.05)
     full = pkg.wind_loss_workspace_bytes(c["w"], N, 0, True)
     assert full < N * V * (6 if dtype == "f32" else 2)          # the gradient's share of logits is not kept whole
-    got, want = call(pkg, c), None
-    # 64-bit reference in slices of rows
-    total = {}
-    for r0 in range(0, N, 20000):
-        rows = slice(r0, min(N, r0 + 20000))
-        part = {k: (v[rows] if k in ("x", "t", "dloss") else v) for k, v in c.items()}
-        want = reference(part)
-        verify({k: got[k][rows] for k in ("loss", "lse", "dx")}, want)
-        for k in ("dw", "db", "tol_dw", "tol_db"):
-            total[k] = total.get(k, 0) + want[k]
-    steps = N / 16 * (6 if dtype == "f32" else 1) * 2.0 ** -23           # sums over all rows, not over a slice
-    for k in ("dw", "db"):
-        d = (got[k].double() - total[k]).abs()
-        assert bool((d <= total["tol_" + k] * (1 + steps * 2.0 ** 9)).all()), k
+    verify_in_slices(call(pkg, c), c, 20000)
 
 
 def test_gradient_against_differences(pkg):
