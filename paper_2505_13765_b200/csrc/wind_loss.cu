@@ -462,8 +462,11 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const RowsParams p) {
 // The products: a persistent tcgen05 GEMM with three epilogues
 // ---------------------------------------------------------------------------
 enum LossMode { FORWARD = 0, LOGITS = 1, PRODUCTS = 2 };
-// Operands: bf16; bf16 with g in two parts, for calls of few rows; fp32 (three parts of every operand).
+// Operands, by the parts of g: bf16; bf16 with g in two parts, for calls of few rows; fp32 (three parts of every operand).
+// Few rows: an error that many rows' sums and norms average out stands alone in one, and the products' time is that of reading W and
+// writing dW, whatever the parts.  (With one part dx and dW of three rows were 0.0029 off, 0.0017 being bf16's own rounding.)
 enum LossKind { BF16 = 1, BF16_FINE = 2, F32 = 3 };
+constexpr int kFineRows = 256;
 
 struct LossGemm {
     LossCtrl* ctrl;
@@ -495,12 +498,15 @@ struct LossGemm {
 // for six products of 128 x 128 x 64 (64 bytes of L2 a cycle and SM; a fetch for each product would be 128).
 template <int MODE, int KIND>
 struct Shape {
-    static constexpr int TN = KIND == F32 ? 128 : 256;                                       // most columns of a tile (BM = 128 rows)
+    // Logits of fp32 models and of calls of few rows: an accumulator takes one K block, whose sum is added up in registers.  Tensor cores
+    // cut where they add; over a long K that is up to 2^-24 an addition, all one way (a single row of H = 1024 had a loss 3e-6 off).
+    static constexpr bool SUMS = KIND == F32 || (KIND == BF16_FINE && MODE != PRODUCTS);
+    static constexpr int TN = SUMS ? 128 : 256;                                              // most columns of a tile (BM = 128 rows)
     static constexpr int A_PARTS = KIND == F32 ? 3 : (KIND == BF16_FINE && MODE == PRODUCTS ? 2 : 1), B_PARTS = KIND == F32 ? 3 : 1;
     static constexpr int TERMS = KIND == F32 ? 6 : A_PARTS;
     // Groups of four epilogue warps (one per tensor-memory lane quadrant), each with its columns of a tile.  A row of logits is a chain
-    // of maxima, exponentials and sums: 16 warps hide more of it than 8 (which is what fp32's sums leave registers for).
-    static constexpr int GROUPS = MODE != PRODUCTS && KIND != F32 ? 4 : 2;
+    // of maxima, exponentials and sums: 16 warps hide more of it than 8 (which is what sums in registers leave room for).
+    static constexpr int GROUPS = MODE != PRODUCTS && !SUMS ? 4 : 2;
     static constexpr int EPI = 128 * GROUPS, THREADS = 64 + EPI, CHUNKS = TN / GROUPS / 32;
     // Part products, smallest first: the parts of A and B of each (fp32: 20 02 11 10 01 00; fine: 10 00).
     static __device__ __forceinline__ constexpr int a_part(int t) { return KIND == F32 ? (0x001102 >> (4 * t)) & 3 : TERMS - 1 - t; }
@@ -730,10 +736,10 @@ __device__ __forceinline__ int unit_cols(const LossGemm& p, const Unit& t) {   /
     return MODE == PRODUCTS ? min(p.tn, p.H - t.nt * p.tn) : min(p.tn, p.cols - t.nt * p.tn);
 }
 
-// 32 columns of an accumulator row: from tensor memory, or (fp32) from the sums in registers.
-template <int KIND>
+// 32 columns of an accumulator row: from tensor memory, or from the sums in registers.
+template <bool SUMS>
 __device__ __forceinline__ void fetch32(float* v, uint32_t taddr, const float* sums, int c) {
-    if constexpr (KIND == F32) {
+    if constexpr (SUMS) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = sums[c * 32 + i];
     } else {
@@ -808,12 +814,13 @@ template <bool LIST, int KIND, int CHUNKS>
 __device__ __forceinline__ RowPart forward_row(const LossGemm& p, uint32_t taddr, const float* sums, const float* bias, int col, int n_cols,
                                                Targets<LIST>& targets) {
     RowPart part{-CUDART_INF_F, 0.f, 0.f};
-    constexpr int UNROLL = KIND == F32 ? CHUNKS : 1;
+    constexpr bool SUMS = Shape<FORWARD, KIND>::SUMS;
+    constexpr int UNROLL = SUMS ? CHUNKS : 1;
 #pragma unroll UNROLL
     for (int c = 0; c < CHUNKS; ++c) {
         if (c * 32 >= n_cols) continue;
         float v[32];
-        fetch32<KIND>(v, taddr, sums, c);
+        fetch32<SUMS>(v, taddr, sums, c);
         float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
         const float4* b4 = reinterpret_cast<const float4*>(bias + c * 32);
 #pragma unroll
@@ -864,14 +871,15 @@ __device__ __forceinline__ void logits_row(const LossGemm& p, const CUtensorMap*
     const int lane = threadIdx.x & 31, col = p.v0 + g_col;
     __nv_bfloat16* dst = p.g + (size_t)row * p.ldg + g_col;
     const int g_end = (p.cols + 63) / 64 * 64 - g_col;
-    constexpr int UNROLL = KIND == F32 ? CHUNKS : 1;
+    constexpr bool SUMS = Shape<LOGITS, KIND>::SUMS;
+    constexpr int UNROLL = SUMS ? CHUNKS : 1;
 #pragma unroll UNROLL
     for (int c = 0; c < CHUNKS; ++c) {
         if (c * 32 >= n_cols || c * 32 >= g_end) continue;
         float v[32];
         const bool some = col + c * 32 < p.n_out;   // (behind the outputs the accumulator holds what an earlier tile left)
         if (some) {
-            fetch32<KIND>(v, taddr, sums, c);
+            fetch32<SUMS>(v, taddr, sums, c);
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
                 const float4 b = reinterpret_cast<const float4*>(bias + c * 32)[i / 4];
@@ -946,7 +954,7 @@ __device__ __forceinline__ void product_row(const LossGemm& p, const Unit& t, fl
         if (zero) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
-        } else fetch32<KIND>(v, taddr, sums, c);
+        } else fetch32<f32>(v, taddr, sums, c);
         if (!slab && !(vec && h + 32 <= h1)) {
             const int lane = threadIdx.x & 31;
             const unsigned long long mine = reinterpret_cast<unsigned long long>(out);
@@ -1071,7 +1079,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const int panels = PAIR ? (half + 63) / 64 : (unit_cols<MODE>(p, t) + 63) / 64;
                 const int a_part = (MODE == PRODUCTS && t.dw ? BM : p.a_rows) * BK * 2;
                 const uint32_t bytes = A_PARTS * a_part + B_PARTS * (MODE == PRODUCTS ? panels * PANEL_BYTES : p.b_bytes);
-                const int hand_at = KIND == F32 || (PAIR && rank) ? -1 : t.k0 + min(t.nk, p.stages) - 1;   // (fp32, and a pair's other CTA: when it is through)
+                const int hand_at = S::SUMS || (PAIR && rank) ? -1 : t.k0 + min(t.nk, p.stages) - 1;   // (sums, and a pair's other CTA: when it is through)
                 for (int kb = t.k0; kb < t.k0 + t.nk; ++kb) {
                     if (!mbar_wait(&empty_bar[s], (turn & 1) ^ 1, &abort_flag)) { ok = false; break; }
                     uint8_t* b = a + A_PARTS * a_part;
@@ -1128,7 +1136,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const uint64_t a0 = a_mn ? major_mn : major_k, b0 = (b_mn ? major_mn : major_k) + A_PARTS * a_part;
                 for (int i = 0; i < t.nk; ++i) {
                     const uint32_t acc = n_acc & 1u;
-                    const bool first = KIND == F32 || i == 0, last = KIND == F32 || i == t.nk - 1;   // of an accumulator
+                    const bool first = S::SUMS || i == 0, last = S::SUMS || i == t.nk - 1;   // of an accumulator
                     if (first) {
                         const uint32_t parity = ((n_acc >> 1) & 1u) ^ 1u;
                         ok = PAIR ? mbar_wait_pair(&acc_empty[acc], parity, &abort_flag) : mbar_wait(&acc_empty[acc], parity, &abort_flag);
@@ -1192,23 +1200,21 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             // One thread asks for the next unit, which is there before this one's accumulator is; all warps hear the same answer, so that
             // they leave together.  (A warp whose wait runs out goes on without waiting: the others still meet it at the barriers.)
-            // fp32 asks when it is through with this one: its operands are not all fetched before that, its accumulators being emptied here.
+            // With sums it asks when it is through with this one: the operands are not all fetched before that, the accumulators being emptied here.
             auto ask = [&] {
                 if (et == 0) write_unit(&s_unit[n_tile & 1], next_unit<PAIR>(units, n_tile, rank, &abort_flag));
                 __syncwarp();
                 asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
                 then = read_unit(&s_unit[n_tile & 1]);
             };
-            if (KIND != F32) ask();
+            if (!S::SUMS) ask();
             else if (MODE != PRODUCTS) {
                 __syncwarp();
                 asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
             }
-            // fp32: an accumulator takes one K block, whose sum is added up here.  (Tensor cores cut where they add; over a long K that
-            // is an error of 2^-25 an addition, all one way: 5e-6 of dW over 20 000 rows.)
-            float sums[KIND == F32 ? S::CHUNKS * 32 : 1];
+            float sums[S::SUMS ? S::CHUNKS * 32 : 1];
             uint32_t taddr = lanes;
-            if constexpr (KIND == F32) {
+            if constexpr (S::SUMS) {
 #pragma unroll
                 for (int i = 0; i < S::CHUNKS * 32; ++i) sums[i] = 0.f;
                 for (int i = 0; i < t.nk; ++i, ++n_acc) {
@@ -1245,7 +1251,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     product_row<KIND, S::CHUNKS>(p, t, reinterpret_cast<float*>(stage), taddr, sums, t.nt * p.tn + my0, row, n_rows, t.nk == 0);
                 }
             }
-            if (KIND != F32 && t.nk > 0) {
+            if (!S::SUMS && t.nk > 0) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
@@ -1278,7 +1284,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const int c = t.nt * p.tn + et;
                 if (et < p.tn && c < p.cols) p.dbp[(size_t)(t.mt * (TM / BM) + rank) * p.ldg + c] = (s_db[0][et] + s_db[1][et]) + (s_db[2][et] + s_db[3][et]);
             }
-            if (KIND == F32) ask();
+            if (S::SUMS) ask();
         }
         if (MODE == LOGITS && KIND == BF16 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
@@ -1456,7 +1462,8 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
     LossLayout L{};
     const bool f32 = o.dtype == WIND_DT_F32;
     L.planes = f32 ? 3 : 1;
-    L.g_planes = f32 ? 3 : N <= 256 ? 2 : 1;
+    L.kind = f32 ? F32 : N <= kFineRows ? BF16_FINE : BF16;
+    L.g_planes = L.kind;
     L.pack_w = f32 || o.H % 8 || o.ldw % 8 || (o.n_out > 1 && o.ldw < o.H) || reinterpret_cast<uintptr_t>(o.w) % 16;
     L.Hp = up(o.H, 64);
     L.Npad = N <= BM ? up(N, BM) : up(N, 2 * BM);
@@ -1464,7 +1471,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
     auto take = [&](size_t bytes) { size_t at = off; off = align_up(off + bytes); return at; };
     L.ctrl = take(sizeof(LossCtrl));
     const size_t np = (size_t)L.Npad;
-    const int most = f32 ? Shape<FORWARD, F32>::TN : Shape<FORWARD, BF16>::TN;
+    const int most = L.kind == BF16 ? Shape<FORWARD, BF16>::TN : Shape<FORWARD, F32>::TN;
     L.counts = take(N > ROWS_COUNTED ? 4 * (size_t)cdiv(N, ROWS_COUNTED) : 0);
     L.mark = take(K ? np : 0);
     L.src = take(4 * np);
@@ -1479,7 +1486,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
     L.w = take(L.pack_w ? 2 * (size_t)L.planes * o.n_out * L.Hp : 0);
     if (!grad) {
         L.tn = tile_cols(L.Npad / BM, o.n_out, most);
-        L.pair = !f32 && pairs_pay(o.H, (long long)(L.Npad / BM) * cdiv(o.n_out, 256));
+        L.pair = L.kind == BF16 && pairs_pay(o.H, (long long)(L.Npad / BM) * cdiv(o.n_out, 256));
         if (L.pair) L.tn = most;
         L.parts = cdiv(o.n_out, L.tn);
         L.next = take(4);
@@ -1496,12 +1503,12 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
         L.piece = (int)std::min(all, std::max(2048LL, fit));
         L.pieces = cdiv(o.n_out, L.piece);
         L.tn = tile_cols(L.Npad / BM, std::min(o.n_out, L.piece), most);
-        L.pair = L.g_planes == 1 && pairs_pay(o.H, (long long)(L.Npad / BM) * cdiv(std::min(o.n_out, L.piece), 256));
+        L.pair = L.kind == BF16 && pairs_pay(o.H, (long long)(L.Npad / BM) * cdiv(std::min(o.n_out, L.piece), 256));
         if (L.pair) L.tn = most;
-        L.tn_products = most;
+        L.tn_products = f32 ? Shape<PRODUCTS, F32>::TN : Shape<PRODUCTS, BF16>::TN;
         const int ht = cdiv(o.H, L.tn_products), terms = f32 ? 6 : 1;
         const long long t_dx = (long long)(L.Npad / BM) * ht, t_dw = (long long)cdiv(std::min(o.n_out, L.piece), BM) * ht;
-        L.pair_products = L.g_planes == 1 && pairs_pay(o.H, t_dx + t_dw);
+        L.pair_products = L.kind == BF16 && pairs_pay(o.H, t_dx + t_dw);
         const int kb_dx = cdiv(std::min(o.n_out, L.piece), BK), kb_dw = L.Npad / BK;
         // Parts of a sum: units of at most two thirds of a CTA's share of all K blocks, so that the units taken last fill the gaps, but of
         // 8 K blocks (bf16) at least, and none where the tiles alone are many.
@@ -1587,10 +1594,7 @@ struct LossLaunch { LossKernel kernel; int threads, a_parts, b_parts, pair; };
 template <int MODE>
 static LossLaunch loss_launch_of(bool list, int kind, bool pair) {
     if (kind == F32) return {loss_kernel_of<MODE, F32, false>(list), Shape<MODE, F32>::THREADS, Shape<MODE, F32>::A_PARTS, Shape<MODE, F32>::B_PARTS, 0};
-    if (MODE != FORWARD && kind == BF16_FINE) {
-        constexpr int M = MODE == FORWARD ? LOGITS : MODE;
-        return {loss_kernel_of<M, BF16_FINE, false>(list), Shape<M, BF16_FINE>::THREADS, Shape<M, BF16_FINE>::A_PARTS, Shape<M, BF16_FINE>::B_PARTS, 0};
-    }
+    if (kind == BF16_FINE) return {loss_kernel_of<MODE, BF16_FINE, false>(list), Shape<MODE, BF16_FINE>::THREADS, Shape<MODE, BF16_FINE>::A_PARTS, 1, 0};
     return {pair ? loss_kernel_of<MODE, BF16, true>(list) : loss_kernel_of<MODE, BF16, false>(list), Shape<MODE, BF16>::THREADS, 1, 1, pair};
 }
 
@@ -1744,7 +1748,7 @@ cudaError_t loss_run(const LossCall& c) {
         p.pm = reinterpret_cast<float*>(c.ws + L.pm);
         p.ps = reinterpret_cast<float*>(c.ws + L.ps);
         p.pq = reinterpret_cast<float*>(c.ws + L.pq);
-        const LossLaunch l = loss_launch_of<FORWARD>(c.K > 0, L.planes, L.pair);
+        const LossLaunch l = loss_launch_of<FORWARD>(c.K > 0, L.kind, L.pair);
         ring_of(p, l, few, L.tn);
         p.next = direct ? nullptr : r.next;
         if (direct) { p.direct = c.N; p.src = nullptr; p.target = c.target; }
@@ -1781,7 +1785,7 @@ cudaError_t loss_run(const LossCall& c) {
         p.n_vt = cdiv(p.cols, L.tn);
         p.add_dx = piece > 0;
         p.dbp = !c.db ? nullptr : one_tile ? c.db + p.v0 : reinterpret_cast<float*>(c.ws + L.dbp);
-        const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, L.g_planes, L.pair);
+        const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, L.kind, L.pair);
         ring_of(p, l, few, L.tn);
         p.next = r.next + 2 * piece;
         if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_store, map_w, p, c.stream)) != cudaSuccess) return e;
@@ -1793,7 +1797,7 @@ cudaError_t loss_run(const LossCall& c) {
             finish_blocks = cdiv(p.cols, 32);
         }
         p.tn = L.tn_products;
-        const LossLaunch lp = loss_launch_of<PRODUCTS>(false, L.g_planes, L.pair_products);
+        const LossLaunch lp = loss_launch_of<PRODUCTS>(false, L.kind, L.pair_products);
         ring_of(p, lp, c.dw ? BM : few, p.tn);
         p.a_rows = few;
         const int tm = lp.pair ? 2 * BM : BM;

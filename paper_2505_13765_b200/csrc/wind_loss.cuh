@@ -26,7 +26,8 @@ struct LossCtrl {
 // How a call is cut up, and the byte offsets of its workspace regions.  Host arithmetic on the sizes alone.
 struct LossLayout {
     int planes;        // bf16 parts of an operand: 1 (bf16) or 3 (fp32)
-    int g_planes;      // of the gradient's share of logits: 1, 2 (bf16, few rows) or 3 (fp32)
+    int kind;          // LossKind
+    int g_planes;      // bf16 parts of the gradient's share of logits: 1, 2 (bf16, few rows) or 3 (fp32)
     int pack_w;        // W is laid out again: fp32, or rows that TMA cannot start on
     int where_ld;      // bytes of a row's index into its list of the teacher's entries
     int Hp, Npad;      // H up to a multiple of 64, N up to a multiple of 128
