@@ -1481,10 +1481,11 @@ static int tile_cols(int row_tiles, int cols, int most) {
 }
 
 // Two CTAs to a tile of 256 x 256 fetch a third less from L2 than a CTA to 128 x 256, and draw less power, but there are half as many
-// tiles to spread over the chip.  A text model's step (4096 rows, H = 2048, 65536 outputs): 3.50 ms against 3.65; the large vocabulary's
-// (H = 1024) is the same either way, the lattice's (H = 640) 138 us against 120.
-constexpr int kPairTiles = 2 * kFillCtas, kPairH = 1536;
-static bool pairs_pay(int H, long long tiles) { return H >= kPairH && tiles >= kPairTiles; }
+// tiles to spread over the chip.  Logits: a text model's step (4096 rows, H = 2048, 65536 outputs) takes 3.50 ms with them and 3.65
+// without, the large vocabulary's logits (H = 1024) 102 us either way, the lattice's (H = 640) 30 us against 26.  Products: the large
+// vocabulary's 180 us against 189 (8003 rows, 512 tiles), 5 us lost with half the rows, the lattice's 47 us against 38.
+static bool pairs_pay(int H, long long tiles) { return H >= 1536 && tiles >= 2 * kFillCtas; }
+static bool pairs_pay_products(int H, long long tiles) { return H >= 1024 && tiles >= 3 * kFillCtas; }
 
 LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most_of_fewer) {
     LossLayout L{};
@@ -1536,7 +1537,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
         L.tn_products = f32 ? Shape<PRODUCTS, F32>::TN : Shape<PRODUCTS, BF16>::TN;
         const int ht = cdiv(o.H, L.tn_products), terms = f32 ? 6 : 1;
         const long long t_dx = (long long)(L.Npad / BM) * ht, t_dw = (long long)cdiv(std::min(o.n_out, L.piece), BM) * ht;
-        L.pair_products = L.kind == BF16 && pairs_pay(o.H, t_dx + t_dw);
+        L.pair_products = L.kind == BF16 && pairs_pay_products(o.H, t_dx + t_dw);
         const int kb_dx = cdiv(std::min(o.n_out, L.piece), BK), kb_dw = L.Npad / BK;
         // Parts of a sum: units of at most two thirds of a CTA's share of all K blocks, so that the units taken last fill the gaps, but of
         // 8 K blocks (bf16) at least, and none where the tiles alone are many.
