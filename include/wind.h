@@ -256,8 +256,13 @@ wind_status_t wind_window_first_output(const wind_model_t* m, const void* enc, c
  *   gradient of sum_r dloss[r] loss_r with regard to x, W and b; with s_r = dloss[r] (distill: tau dloss[r]) and
  *            g_rv = s_r (p_rv - [sum of the q_rk with i(r, k) = v])  (labels: q is 1 at the target):  dx = g W, dW = g^T x, db = sum_r g_r
  *
- * Unlike the decoding calls these only enqueue work (they may be captured into a graph): wind_loss_status waits and returns what
- * the device found.
+ * Unlike the decoding calls these only enqueue work (they may be captured into a graph, from the second call of a process on a device
+ * on: the first one loads the kernels): wind_loss_status waits and returns what the device found.
+ *
+ * Arithmetic: logits, exponentials, sums, lse, loss and db in fp32.  bf16 models: products of bf16 operands, g rounded to bf16 (to two
+ * bf16 parts, 16 bits, in calls of up to 256 rows), dx and dW rounded to bf16 once.  fp32 models: every operand as the sum of three bf16
+ * parts, and the part products above 2^-24 of a product, on the tensor cores; an infinite operand gives NaN there where fp32
+ * arithmetic gives an infinity.
  */
 typedef struct {
     int32_t n_out, H;          /* outputs (V + 1 of a model), activations */

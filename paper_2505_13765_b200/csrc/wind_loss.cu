@@ -10,20 +10,33 @@
 //     loss_list     the teacher's entries of a row to probabilities, sorted by label
 //     loss_gather   rows that count, one behind the other, as tensor-core operands: padding costs nothing from here on; W as a
 //                   tensor-core operand, where it is not one already
-//     loss_gemm     FORWARD   128 x 256 tiles of logits on the tensor cores; of each tile's row only (maximum, sum of exponentials,
-//                             sum of q z) leave the chip
+//     loss_gemm     FORWARD   tiles of logits on the tensor cores; of each tile's row only (maximum, sum of exponentials, sum of q z)
+//                             leave the chip
 //                   LOGITS    the same tiles again, turned into g, for a piece of the outputs
 //                   PRODUCTS  dx += g W and dW = g^T x of that piece, g as both operands' layouts need it: rows are contiguous along
 //                             the outputs, which is K of the first product and M of the second (the matrix descriptors take either)
 //     loss_combine  a row's partial results to its loss and log-sum-exp
 //     loss_finish   partial sums of dx / dW, where a product is cut along its K to fill the chip; db
 //
-// fp32 operands are cut into three bf16 parts, x = x1 + x2 + x3 with 8 bits each, and a product into the six of nine part products
-// that are not below 2^-24 of it: x1 w1 + (x1 w2 + x2 w1) + (x1 w3 + x2 w2 + x3 w1), smallest first, in one fp32 accumulator.
-// That is fp32 arithmetic at a sixth of the bf16 rate, three times the rate of the fp32 units.
+// Tiles: 128 x 256 of bf16 (narrower where that fills the chip better), 256 x 256 by two CTAs for wide rows and many tiles, 128 x 128
+// of fp32 and of up to 256 rows.  g in pieces of the outputs and the logits made twice: keeping all of g, or the logits between the two
+// calls, would take 2 N n_out bytes, and making logits again costs a quarter of a step's products.
 //
-// Rounding: logits, exponentials, sums and db stay in fp32.  g is rounded to bf16 (three parts of it for fp32 models) because it is a
-// tensor-core operand; dx and dW are accumulated in fp32 and rounded once.
+// fp32 operands are cut into three bf16 parts, x = x1 + x2 + x3 with 8 bits each, and a product into the six of nine part products
+// that are not below 2^-24 of it: x1 w1 + (x1 w2 + x2 w1) + (x1 w3 + x2 w2 + x3 w1), smallest first, in one fp32 accumulator per K
+// block.  That is fp32 arithmetic at a sixth of the bf16 rate: 1999 rows, H = 640, 1025 outputs go through their four products at 104
+// TFLOP/s of fp32 over the whole step, launches, parts and sums included (the fp32 units' nominal peak is 74.5).
+//
+// Rounding: logits, exponentials, sums and db stay in fp32.  g is rounded to bf16 (two parts of it up to 256 rows, three for fp32
+// models) because it is a tensor-core operand; dx and dW are accumulated in fp32 and rounded once.
+//
+// What bounds it, loss and gradient together (B200; floor: 8 N H n_out operations at a large matrix product's 1625 TFLOP/s):
+//     4096 rows, H = 2048, 65536 outputs     3.4 to 3.5 ms, floor 2.7: the tensor cores under the power limit (3.2 at the rate that a
+//                                            matrix product keeps up for seconds)
+//     8003 rows, H = 1024, 8193 outputs      460 to 470 us, floor 298: the same, the epilogue of LOGITS, and last waves of equal tiles
+//     20011 rows (35 % padding), 640, 1025   114 to 118 us, floor 42: FORWARD 21, LOGITS 26 (exponentials and rounding, 6700 cycles a tile
+//                                            against 5200 of products), PRODUCTS 38, gathering 2 x 13 at 2.5 TB/s, joining and sums 11
+//     1 row, 1024, 8193 (loss)               12 us, floor 2.6: two launches, W read at 5 TB/s
 //
 // Every wait on an mbarrier is bounded: after about two seconds the CTA flags WIND_ERR_TIMEOUT, frees its tensor memory and returns.
 #include <cuda.h>
@@ -90,64 +103,94 @@ constexpr int WHERE_WORDS = 512;
 constexpr uint32_t NO_LABEL = 0xffffffu;   // (n_out is below 2^24)
 
 // The teacher's list of a row, a warp each: probabilities over the entries that are there, and the entries by rising label (equal
-// labels in their order), so that the epilogues walk a list along their columns.  The place of an entry is the number of keys
-// label * 256 + entry below its own: K^2 / 32 comparisons a lane.  `where` has for every 32nd output the number of entries below it (255
-// for 256), a byte each: the epilogues start there (searching, 16 warps a tile, cost them 4000 cycles a tile).
+// labels in their order), so that the epilogues walk a list along their columns: the keys label * 256 + entry, PER to a lane, go through
+// a bitonic network of exchanges between lanes.  (Finding a key's place by counting the keys below it is K^2 / 32 comparisons a lane:
+// 38 us instead of 23 for 19677 lists of 74, 36 instead of 14 for 9924 of 115, 7.0 instead of 5.9 for 6007 of 16.)  `where` has for every
+// 32nd output the number of entries below it (255 for 256), a byte each: the epilogues start there (searching, 16 warps a tile, cost
+// them 4000 cycles a tile).
+template <int PER>
 __global__ void __launch_bounds__(256) loss_list_kernel(const RowsParams p) {
-    __shared__ __align__(16) uint32_t s_keys[8][kLossMaxK], s_where[8][WHERE_WORDS];
+    __shared__ __align__(16) uint32_t s_where[8][WHERE_WORDS];
+    __shared__ float s_q[8][32 * PER];
     let_next_start();
     wait_for_previous();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r = blockIdx.x * 8 + warp;
     if (r >= p.N) return;
-    uint32_t* keys = s_keys[warp];
     const int32_t* ids = p.ids + (size_t)r * p.K;
     const float* y = p.y + (size_t)r * p.K;
+    uint32_t key[PER];
+    float v[PER];
+    int id[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = lane + 32 * i;
+        id[i] = k < p.K ? ids[k] : -1;
+        v[i] = k < p.K ? y[k] : 0.f;
+    }
     float top = -CUDART_INF_F;
     int flags = 0;   // 1: an entry outside the outputs, 2: NaN
-    for (int k = lane; k < (p.K + 3) / 4 * 4; k += 32) {
-        uint32_t key = 0xffffffffu;      // (behind the list: below no key)
-        if (k < p.K) {
-            const int id = ids[k];
-            const float v = y[k];
-            if (id < -1 || id >= p.n_out) flags |= 1;
-            const bool there = id >= 0 && id < p.n_out;
-            if (there && v != v) flags |= 2;
-            if (there) top = fmaxf(top, v);
-            key = (there ? (uint32_t)id : NO_LABEL) << 8 | (uint32_t)k;
-        }
-        keys[k] = key;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const bool there = id[i] >= 0 && id[i] < p.n_out;
+        if (id[i] < -1 || id[i] >= p.n_out) flags |= 1;
+        if (there && v[i] != v[i]) flags |= 2;
+        if (there) top = fmaxf(top, v[i]);
+        else v[i] = -CUDART_INF_F;
+        key[i] = lane + 32 * i < p.K ? (there ? (uint32_t)id[i] : NO_LABEL) << 8 | (uint32_t)(lane + 32 * i) : 0xffffffffu;   // (behind the list: below no key)
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        flags |= __shfl_xor_sync(0xffffffffu, flags, o);
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    flags = __reduce_or_sync(0xffffffffu, flags);
+    float sum = 0.f, e[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const bool some = v[i] != -CUDART_INF_F;
+        v[i] = some ? (v[i] - top) / p.tau : 0.f;
+        e[i] = some ? expf(v[i]) : 0.f;
+        sum += e[i];
     }
-    __syncwarp();
-    float sum = 0.f;
-    for (int k = lane; k < p.K; k += 32)
-        if (keys[k] >> 8 != NO_LABEL && y[k] != -CUDART_INF_F) sum += expf((y[k] - top) / p.tau);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float log_sum = logf(sum);
     float ent = 0.f;
-    for (int k = lane; k < p.K; k += 32) {
-        const uint32_t key = keys[k];
-        float q = 0.f;
-        if (key >> 8 != NO_LABEL && y[k] != -CUDART_INF_F) {
-            const float d = (y[k] - top) / p.tau;
-            q = expf(d) / sum;
-            if (q != 0.f) ent += q * (d - log_sum);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const float q = e[i] != 0.f ? e[i] / sum : 0.f;
+        if (q != 0.f) ent += q * (v[i] - log_sum);
+        s_q[warp][lane + 32 * i] = q;
+    }
+    // position of a key in the network: lane * PER + i
+#pragma unroll
+    for (int size = 2; size <= 32 * PER; size *= 2) {
+#pragma unroll
+        for (int stride = size / 2; stride > 0; stride /= 2) {
+            if (stride >= PER) {
+                const bool low = ((lane & (stride / PER)) == 0) == ((lane * PER & size) == 0);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const uint32_t other = __shfl_xor_sync(0xffffffffu, key[i], stride / PER);
+                    key[i] = low ? min(key[i], other) : max(key[i], other);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    if (i & stride) continue;
+                    const bool rising = ((lane * PER + i) & size) == 0;
+                    const uint32_t a = key[i], b = key[i + stride];
+                    key[i] = rising ? min(a, b) : max(a, b);
+                    key[i + stride] = rising ? max(a, b) : min(a, b);
+                }
+            }
         }
-        int place = 0;
-#pragma unroll 4
-        for (int j = 0; j < p.K; j += 4) {
-            const uint4 o = *reinterpret_cast<const uint4*>(keys + j);
-            place += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
-        }
-        const int label = key >> 8 == NO_LABEL ? 0x7fffffff : (int)(key >> 8);
-        p.list[(size_t)r * p.K + place] = make_int2(label, __float_as_int(q));
-        if (place == 255) keys[k] = 0xffffffffu;       // (never the reason to start behind entry 255)
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int at = lane * PER + i;
+        const int label = key[i] >> 8 == NO_LABEL ? 0x7fffffff : (int)(key[i] >> 8);
+        if (at < p.K) p.list[(size_t)r * p.K + at] = make_int2(label, __float_as_int(s_q[warp][key[i] & 255]));
+        if (at == 255) key[i] = 0xffffffffu;       // (never the reason to start behind entry 255)
     }
     // `where`: how many labels lie in each 32 outputs, a byte each, and their running sums
     uint32_t* w = s_where[warp];
@@ -157,10 +200,10 @@ __global__ void __launch_bounds__(256) loss_list_kernel(const RowsParams p) {
         __syncwarp();
         for (int i = lane; i < words; i += 32) w[i] = 0;
         __syncwarp();
-        for (int k = lane; k < p.K; k += 32) {
-            const uint32_t key = keys[k];
-            const int at = (int)(key >> 13) + 1 - b0;      // label / 32 + 1
-            if (key >> 8 != NO_LABEL && at >= 0 && at < 4 * words) atomicAdd(&w[at >> 2], 1u << (8 * (at & 3)));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = (int)(key[i] >> 13) + 1 - b0;      // label / 32 + 1
+            if (key[i] >> 8 != NO_LABEL && at >= 0 && at < 4 * words) atomicAdd(&w[at >> 2], 1u << (8 * (at & 3)));
         }
         __syncwarp();
         for (int i0 = 0; i0 < words; i0 += 32) {
@@ -555,11 +598,17 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 constexpr float kLog2e = 1.4426950408889634f;
 
+// v[at], by halves: 31 selections and five comparisons (a comparison and a selection for each value: FORWARD of 6007 rows with 16
+// entries 15.2 us instead of 14.6)
 __device__ __forceinline__ float pick32(const float* v, int at) {
-    float x = 0.f;
+    float t[16];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) x = at == i ? v[i] : x;
-    return x;
+    for (int i = 0; i < 16; ++i) t[i] = (at & 16) ? v[i + 16] : v[i];
+#pragma unroll
+    for (int h = 8; h > 0; h >>= 1)
+#pragma unroll
+        for (int i = 0; i < h; ++i) t[i] = (at & h) ? t[i + h] : t[i];
+    return t[0];
 }
 
 // What a CTA's roles need to know about a piece of work.
@@ -1750,7 +1799,8 @@ cudaError_t loss_run(const LossCall& c) {
     r.xc = reinterpret_cast<__nv_bfloat16*>(c.ws + L.x);
     r.loss = c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.dloss; r.dx = c.dx; r.lddx = c.lddx;
     if (c.K) {
-        if ((e = launch_small(loss_list_kernel, cdiv(c.N, 8), c.stream, r)) != cudaSuccess) return e;
+        void (*list)(RowsParams) = c.K <= 32 ? loss_list_kernel<1> : c.K <= 64 ? loss_list_kernel<2> : c.K <= 128 ? loss_list_kernel<4> : loss_list_kernel<8>;
+        if ((e = launch_small(list, cdiv(c.N, 8), c.stream, r)) != cudaSuccess) return e;
     }
     r.counted = c.N > ROWS_COUNTED;
     if (r.counted) {

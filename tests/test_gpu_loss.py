@@ -294,6 +294,15 @@ def test_full_lists_of_low_labels(pkg, N):
     verify(call(pkg, c), reference(c))
 
 
+@pytest.mark.parametrize("K", [2, 31, 32, 34, 63, 64, 65, 127, 128, 129, 255])
+def test_lengths_of_lists(pkg, K):
+    """Lists around the lengths at which a lane takes more entries, few labels (many entries of one label) and many."""
+    for V in (17, 9000):
+        for full in (False, True):
+            c = make(40 + K, "f32", 37, 24, V, K, pad=0.1, full=full)
+            verify(call(pkg, c), reference(c), (V, full))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("K", [0, 5])
 def test_vectors_that_start_anywhere(pkg, dtype, K):
