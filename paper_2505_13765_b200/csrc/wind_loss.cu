@@ -35,7 +35,7 @@
 //                                            matrix product keeps up for seconds)
 //     8003 rows, H = 1024, 8193 outputs      460 to 470 us, floor 298: the same, the epilogue of LOGITS, and last waves of equal tiles
 //     20011 rows (35 % padding), 640, 1025   114 to 118 us, floor 42: FORWARD 21, LOGITS 26 (exponentials and rounding, 6700 cycles a tile
-//                                            against 5200 of products), PRODUCTS 38, gathering 2 x 13 at 2.5 TB/s, joining and sums 11
+//                                            against 5200 of products), PRODUCTS 38, gathering 2 x 11.5 at 2.9 TB/s, joining and sums 11
 //     1 row, 1024, 8193 (loss)               12 us, floor 2.6: two launches, W read at 5 TB/s
 //
 // Every wait on an mbarrier is bounded: after about two seconds the CTA flags WIND_ERR_TIMEOUT, frees its tensor memory and returns.
@@ -1806,7 +1806,9 @@ cudaError_t loss_run(const LossCall& c) {
     if (r.counted) {
         if ((e = launch_small(loss_count_kernel, cdiv(c.N, ROWS_COUNTED), c.stream, r)) != cudaSuccess) return e;
     }
-    r.per_block = std::min(256, up(cdiv(c.N, 8 * sms), 8));   // one wave of blocks (8 an SM), while they are not too long
+    // Two blocks an SM, while they are not too long: each counts the rows before its own (20011 rows of H = 640: 11.5 us; with 4 to 6 an SM
+    // 12 to 14, with one of 1024 threads 11.3; with x fetched before counting the same)
+    r.per_block = std::min(256, up(cdiv(c.N, 2 * sms), 8));
     r.row_blocks = cdiv(c.N, r.per_block);
     const void* w = c.o.w;
     int64_t ldw = c.o.ldw;
