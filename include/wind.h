@@ -285,7 +285,7 @@ wind_status_t wind_loss_workspace_bytes(const wind_output_t* o, int32_t N, int32
 
 /*
  * Loss and log-sum-exp (of z / tau) of N rows against labels.
- *   x       [N, H], rows ldx elements apart (any distance and alignment; 0: the same row)
+ *   x       [N, H], rows ldx elements apart (any distance, any address that is one of an element; 0: the same row)
  *   target  [N] int32 in [0, n_out), or -1: a row of padding.  Its loss and lse are 0 and its x is not read (it may hold NaN).
  *           With another value loss and lse of that row are NaN, no output is read through it and the status is WIND_ERR_INVALID_ARG.
  *   loss, lse  [N] fp32

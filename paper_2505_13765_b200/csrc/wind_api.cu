@@ -500,6 +500,12 @@ static wind_status_t enqueue_loss(LossCall& c, const wind_output_t* o, const voi
     if (N > 0 && !x) return WIND_ERR_INVALID_ARG;
     if (c.grad && ((c.dx && c.lddx < o->H) || (c.dw && c.lddw < o->H))) return WIND_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) % kAlign) return WIND_ERR_WORKSPACE;
+    // (the kernels read and write whole elements)
+    const uintptr_t of_model = reinterpret_cast<uintptr_t>(o->w) | reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(c.dx) | reinterpret_cast<uintptr_t>(c.dw);
+    const uintptr_t words = reinterpret_cast<uintptr_t>(o->b) | reinterpret_cast<uintptr_t>(c.target) | reinterpret_cast<uintptr_t>(c.ids) |
+                            reinterpret_cast<uintptr_t>(c.y) | reinterpret_cast<uintptr_t>(c.loss) | reinterpret_cast<uintptr_t>(c.lse_out) |
+                            reinterpret_cast<uintptr_t>(c.lse) | reinterpret_cast<uintptr_t>(c.dloss) | reinterpret_cast<uintptr_t>(c.db);
+    if (of_model % (o->dtype == WIND_DT_F32 ? 4 : 2) || words % 4) return WIND_ERR_INVALID_ARG;
     c.o = *o;
     c.x = x; c.ldx = ldx; c.N = N; c.K = K; c.tau = tau;
     c.lay = loss_layout(*o, N, K, c.grad);

@@ -89,6 +89,16 @@ def test_calls_are_refused_before_any_launch(lib):
         refused(f, args, len(args) - 2, 100, bd.WIND_ERR_WORKSPACE)
         for bad in (dict(w=None), dict(n_out=0), dict(H=-3), dict(dtype=7), dict(ldw=-640)):
             refused(f, args, 0, C.byref(layer(**bad)))
+    # addresses that are none of an element's
+    for f, args, vectors, matrices in ((lib.wind_label_loss, lab, (3, 5, 6), (1,)), (lib.wind_label_loss_grad, grad, (3, 5, 6, 11), (1, 7, 9)),
+                                       (lib.wind_distill_loss, dist, (3, 4, 8, 9), (1,)),
+                                       (lib.wind_distill_loss_grad, dgrad, (3, 4, 8, 9, 14), (1, 10, 12))):
+        for at in vectors:
+            refused(f, args, at, p + 2)
+        for at in matrices:
+            refused(f, args, at, p + 1)
+            refused(f, [C.byref(layer(dtype=bd.WIND_DT_F32))] + args[1:], at, p + 2)
+        refused(f, args, 0, C.byref(layer(w=(1 << 20) + 1)))
     refused(lib.wind_label_loss, lab, 5, None)
     refused(lib.wind_label_loss, lab, 6, None)
     refused(lib.wind_label_loss_grad, grad, 5, None)                # lse
