@@ -33,8 +33,8 @@
 // What bounds it, loss and gradient together (B200; floor: 8 N H n_out operations at a large matrix product's 1625 TFLOP/s):
 //     4096 rows, H = 2048, 65536 outputs     3.4 to 3.5 ms, floor 2.7: the tensor cores under the power limit (3.2 at the rate that a
 //                                            matrix product keeps up for seconds)
-//     8003 rows, H = 1024, 8193 outputs      460 to 470 us, floor 298: the same, the epilogue of LOGITS, and last waves of equal tiles
-//     20011 rows (35 % padding), 640, 1025   114 to 118 us, floor 42: FORWARD 21, LOGITS 26 (exponentials and rounding, 6700 cycles a tile
+//     8003 rows, H = 1024, 8193 outputs      455 to 465 us, floor 298: the same, the epilogue of LOGITS, and last waves of equal tiles
+//     20011 rows (35 % padding), 640, 1025   112 us, floor 42: FORWARD 21, LOGITS 26 (exponentials and rounding, 6700 cycles a tile
 //                                            against 5200 of products), PRODUCTS 38, gathering 2 x 11.5 at 2.9 TB/s, joining and sums 11
 //     1 row, 1024, 8193 (loss)               12 us, floor 2.6: two launches, W read at 5 TB/s
 //
