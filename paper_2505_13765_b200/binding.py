@@ -632,62 +632,66 @@ def _check_loss_call(x, weight, bias, rows, forward, backward, workspace, stream
     _need(stream is None or stream.device == dev, f"stream: not on {dev}")
 
 
+class _Unlike(Exception):
+    """A tensor of a loss call is not what the call takes."""
+
+
+def _matrix_arg(t, rows: int, cols: int, dtype, dev: int):
+    """Address and row distance of a matrix whose rows may be any distance apart."""
+    if t.shape == (rows, cols) and t.dtype is dtype and t.get_device() == dev:
+        d, s = t.stride()
+        if s == 1 or cols == 1 or not rows:
+            return t.data_ptr(), d if rows > 1 else cols
+    raise _Unlike
+
+
+def _vector_arg(t, shape, dtype, dev: int):
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise _Unlike
+
+
 def _loss_call(name: str, x, weight, bias, rows, forward, backward, workspace, stream, check: bool) -> int:
     """rows: (target,) or (ids, teacher, tau); forward: (loss, lse) or None; backward: (lse, dloss, dx, dw, db) or None."""
-    torch = _ready()
+    torch = _torch_ready or _ready()
     f32, i32, dt, dev = torch.float32, torch.int32, weight.dtype, weight.get_device()
-    ok = True
-
-    def matrix(t, shape):
-        nonlocal ok
-        d, s = t.stride() if t.dim() == 2 else (0, 0)
-        ok = ok and t.shape == shape and t.dtype is dt and t.get_device() == dev and (s == 1 or shape[1] == 1 or not shape[0])
-        return (t.data_ptr(), d if shape[0] > 1 else shape[1]) if ok else (0, 0)
-
-    def vector(t, shape, dtype, needed=True):
-        nonlocal ok
-        if t is None:
-            ok = ok and not needed
-            return None
-        ok = ok and t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()
-        return t.data_ptr()
-
-    if weight.dim() != 2 or x.dim() != 2 or dev < 0 or not (dt is torch.bfloat16 or dt is f32):
-        ok, n_out, H, N = False, 0, 0, 0
-    else:
-        (n_out, H), N = weight.shape, x.shape[0]
-    w, ldw = matrix(weight, (n_out, H))
-    o = wind_output_t(n_out, H, WIND_DT_F32 if dt is f32 else WIND_DT_BF16, 0, w, ldw, vector(bias, (n_out,), f32, False))
-    args = [C.byref(o), *matrix(x, (N, H))]
-    if len(rows) == 1:
-        args += (vector(rows[0], (N,), i32), N)
-    else:
-        ids, teacher, tau = rows
-        K = ids.shape[1] if ids.dim() == 2 else -1
-        args += (vector(ids, (N, K), i32), vector(teacher, (N, K), f32), N, K, tau)
-    if forward is not None:
-        args += (vector(forward[0], (N,), f32), vector(forward[1], (N,), f32))
-    else:
-        lse, dloss, dx, dw, db = backward
-        args += (vector(lse, (N,), f32), vector(dloss, (N,), f32, False))
-        args += (None, 0) if dx is None else matrix(dx, (N, H))
-        args += (None, 0) if dw is None else matrix(dw, (n_out, H))
-        args.append(vector(db, (n_out,), f32, False))
-    at = workspace.data_ptr()
-    up = -at % 256
-    ok = ok and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == dev
-    ok = ok and (stream is None or stream.device_index == dev)
-    if not ok:
+    try:
+        if dev < 0 or not (dt is torch.bfloat16 or dt is f32):
+            raise _Unlike
+        (n_out, H), (N, _) = weight.shape, x.shape
+        w, ldw = _matrix_arg(weight, n_out, H, dt, dev)
+        px, ldx = _matrix_arg(x, N, H, dt, dev)
+        of_rows = (N,)
+        o = wind_output_t(n_out, H, WIND_DT_F32 if dt is f32 else WIND_DT_BF16, 0, w, ldw, None if bias is None else _vector_arg(bias, (n_out,), f32, dev))
+        if len(rows) == 1:
+            args = (C.byref(o), px, ldx, _vector_arg(rows[0], of_rows, i32, dev), N)
+        else:
+            ids, teacher, tau = rows
+            of_lists = (N, K) = N, ids.shape[1]
+            args = (C.byref(o), px, ldx, _vector_arg(ids, of_lists, i32, dev), _vector_arg(teacher, of_lists, f32, dev), N, K, tau)
+        if forward is not None:
+            args += (_vector_arg(forward[0], of_rows, f32, dev), _vector_arg(forward[1], of_rows, f32, dev))
+        else:
+            lse, dloss, dx, dw, db = backward
+            args += (_vector_arg(lse, of_rows, f32, dev), None if dloss is None else _vector_arg(dloss, of_rows, f32, dev),
+                     *((None, 0) if dx is None else _matrix_arg(dx, N, H, dt, dev)), *((None, 0) if dw is None else _matrix_arg(dw, n_out, H, dt, dev)),
+                     None if db is None else _vector_arg(db, (n_out,), f32, dev))
+        at, size = workspace.data_ptr(), workspace.numel()
+        if workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
+            raise _Unlike
+        if stream is not None and stream.device_index != dev:
+            raise _Unlike
+    except (_Unlike, AttributeError, ValueError, IndexError):
         _check_loss_call(x, weight, bias, rows, forward, backward, workspace, stream)
-        raise ValueError("arguments of the wrong kind")
+        raise ValueError("arguments of the wrong kind") from None
+    up = -at % 256
     raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    args += (at + up, workspace.numel() - up, raw)
-    f = getattr(load_library(), name)
+    f = getattr(_lib or load_library(), name)
     if torch._C._cuda_getDevice() == dev:
-        st = f(*args)
+        st = f(*args, at + up, size - up, raw)
     else:
         with torch.cuda.device(dev):
-            st = f(*args)
+            st = f(*args, at + up, size - up, raw)
     if st != WIND_OK:
         raise WindError(st)
     return wind_loss_status(workspace, stream) if check else st
