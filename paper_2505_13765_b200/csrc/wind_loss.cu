@@ -508,8 +508,11 @@ enum LossMode { FORWARD = 0, LOGITS = 1, PRODUCTS = 2 };
 // Operands, by the parts of g: bf16; bf16 with g in two parts, for calls of few rows; fp32 (three parts of every operand).
 // Few rows: an error that many rows' sums and norms average out stands alone in one, and the products' time is that of reading W and
 // writing dW, whatever the parts.  (With one part dx and dW of three rows were 0.0029 off, 0.0017 being bf16's own rounding.)
-enum LossKind { BF16 = 1, BF16_FINE = 2, F32 = 3 };
+// BF16_LONG: BF16 for logits of more than kLongBlocks K blocks; its products and its one part of g are BF16's.
+enum LossKind { BF16 = 1, BF16_FINE = 2, F32 = 3, BF16_LONG = 4 };
+__host__ __device__ constexpr int parts_of_g(int kind) { return kind == BF16_LONG ? 1 : kind; }
 constexpr int kFineRows = 256;
+constexpr int kLongBlocks = 16;   // K blocks that an accumulator of bf16 logits takes: 64 additions
 
 struct LossGemm {
     LossCtrl* ctrl;
@@ -523,7 +526,7 @@ struct LossGemm {
     int v0, cols, n_vt;           // this piece's first output, its outputs (to n_out at most) and tiles
     int32_t* next;                // units that were taken, beyond the CTAs' first ones; null: CTAs take them in turn
     int direct;                   // FORWARD: x as the caller has it, this many rows; 0: gathered rows
-    float rtau, whole;            // 1 / tau; what makes up for what a sum of logits lost in the tensor cores (see cut_share)
+    float rtau;                   // 1 / tau
     const float* bias;
     const int32_t* src; const int32_t* target; const int2* list; const uint8_t* where; int where_ld;
     float *pm, *ps, *pq;          // FORWARD: [parts][Npad]; where a row has one part its results instead:
@@ -542,10 +545,13 @@ struct LossGemm {
 // for six products of 128 x 128 x 64 (64 bytes of L2 a cycle and SM; a fetch for each product would be 128).
 template <int MODE, int KIND>
 struct Shape {
-    // Logits of fp32 models and of calls of few rows: an accumulator takes one K block, whose sum is added up in registers.  Tensor cores
-    // cut where they add; over a long K that is up to 2^-24 an addition, all one way (a single row of H = 1024 had a loss 3e-6 off).
-    static constexpr bool SUMS = KIND == F32 || (KIND == BF16_FINE && MODE != PRODUCTS);
-    static constexpr int TN = SUMS ? 128 : 256;                                              // most columns of a tile (BM = 128 rows)
+    // Tensor cores cut where they add; over a long K that is up to 2^-24 an addition, all one way (a single row of H = 1024 had a loss
+    // 3e-6 off).  Logits of fp32 models and of calls of few rows: an accumulator takes one K block, whose sum is added up in registers;
+    // logits of long bf16 rows: sixteen of them, which takes FORWARD of 4096 x 2048 x 65536 from 648 to 673 us, LOGITS from 700 to 755 (eight
+    // epilogue warps have room for the sums, sixteen do not); with eight K blocks an accumulator 717 and 852.
+    static constexpr bool SUMS = KIND == F32 || ((KIND == BF16_FINE || KIND == BF16_LONG) && MODE != PRODUCTS);
+    static constexpr int ACC_BLOCKS = SUMS ? (KIND == BF16_LONG ? kLongBlocks : 1) : 1 << 30;         // K blocks that an accumulator takes
+    static constexpr int TN = SUMS && KIND != BF16_LONG ? 128 : 256;                         // most columns of a tile (BM = 128 rows)
     static constexpr int A_PARTS = KIND == F32 ? 3 : (KIND == BF16_FINE && MODE == PRODUCTS ? 2 : 1), B_PARTS = KIND == F32 ? 3 : 1;
     static constexpr int TERMS = KIND == F32 ? 6 : A_PARTS;
     // Groups of four epilogue warps (one per tensor-memory lane quadrant), each with its columns of a tile.  A row of logits is a chain
@@ -896,7 +902,7 @@ __device__ __forceinline__ RowPart forward_row(const LossGemm& p, uint32_t taddr
             const float4 b = b4[i / 4];
             const float bb[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[i + k] = fmaf(v[i + k], p.whole, bb[k]) * p.rtau;
+            for (int k = 0; k < 4; ++k) v[i + k] = (v[i + k] + bb[k]) * p.rtau;
 #pragma unroll
             for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], v[i + k]);
         }
@@ -955,7 +961,7 @@ __device__ __forceinline__ void logits_row(const LossGemm& p, const CUtensorMap*
                 const float4 b = reinterpret_cast<const float4*>(bias + c * 32)[i / 4];
                 const float bb[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[i + k] = scale * exp2_fast((fmaf(v[i + k], p.whole, bb[k]) * p.rtau - nlse) * kLog2e);
+                for (int k = 0; k < 4; ++k) v[i + k] = scale * exp2_fast(((v[i + k] + bb[k]) * p.rtau - nlse) * kLog2e);
             }
             targets.in(col + c * 32, [&](int at, float q) {
 #pragma unroll
@@ -966,7 +972,7 @@ __device__ __forceinline__ void logits_row(const LossGemm& p, const CUtensorMap*
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
         }
-        if constexpr (KIND == BF16) {
+        if constexpr (parts_of_g(KIND) == 1) {
             const uint32_t at = smem_u32(stage) + lane * 32, swap = (lane & 4) << 2;
             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             __syncwarp();
@@ -987,7 +993,7 @@ __device__ __forceinline__ void logits_row(const LossGemm& p, const CUtensorMap*
             store16<1>(dst + c * 32 + 16, 0, v + 16);
         } else {
 #pragma unroll
-            for (int i = 0; i < 32; i += 16) store16<KIND>(dst + c * 32 + i, p.g_plane, v + i);
+            for (int i = 0; i < 32; i += 16) store16<parts_of_g(KIND)>(dst + c * 32 + i, p.g_plane, v + i);
         }
         if (p.dbp) {
             __syncwarp();
@@ -1213,7 +1219,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const uint64_t a0 = a_mn ? major_mn : major_k, b0 = (b_mn ? major_mn : major_k) + A_PARTS * a_part;
                 for (int i = 0; i < t.nk; ++i) {
                     const uint32_t acc = n_acc & 1u;
-                    const bool first = S::SUMS || i == 0, last = S::SUMS || i == t.nk - 1;   // of an accumulator
+                    const bool first = i % S::ACC_BLOCKS == 0, last = i % S::ACC_BLOCKS == S::ACC_BLOCKS - 1 || i == t.nk - 1;   // of an accumulator
                     if (first) {
                         const uint32_t parity = ((n_acc >> 1) & 1u) ^ 1u;
                         ok = PAIR ? mbar_wait_pair(&acc_empty[acc], parity, &abort_flag) : mbar_wait(&acc_empty[acc], parity, &abort_flag);
@@ -1294,21 +1300,35 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             if constexpr (S::SUMS) {
 #pragma unroll
                 for (int i = 0; i < S::CHUNKS * 32; ++i) sums[i] = 0.f;
-                for (int i = 0; i < t.nk; ++i, ++n_acc) {
+                for (int i = 0; i < t.nk; i += S::ACC_BLOCKS, ++n_acc) {
                     const uint32_t acc = n_acc & 1u;
                     ok = ok && mbar_wait_warp(&acc_full[acc], (n_acc >> 1) & 1u, &abort_flag);
                     __syncwarp();
                     tc_fence_after();
 #pragma unroll
                     for (int c = 0; c < S::CHUNKS; ++c) {
-                        float v[32];
-                        tmem_ld32(lanes + acc * TN + c * 32, v);
+                        if constexpr (KIND == BF16_LONG) {
+                            // (with 32 values at a time more of the sums go to local memory)
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) sums[c * 32 + e] += v[e];
+                            for (int h = 0; h < 32; h += 16) {
+                                float v[16];
+                                tmem_ld16(lanes + acc * TN + c * 32 + h, v);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) sums[c * 32 + h + e] += v[e];
+                            }
+                        } else {
+                            float v[32];
+                            tmem_ld32(lanes + acc * TN + c * 32, v);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) sums[c * 32 + e] += v[e];
+                        }
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+                    if (lane == 0) {
+                        if (PAIR && rank) mbar_arrive_at(cl_map(smem_u32(&acc_empty[acc]), 0));
+                        else mbar_arrive(&acc_empty[acc]);
+                    }
                 }
             } else if (t.nk > 0) {
                 const uint32_t acc = n_acc & 1u;
@@ -1363,7 +1383,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             if (S::SUMS) ask();
         }
-        if (MODE == LOGITS && KIND == BF16 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (MODE == LOGITS && parts_of_g(KIND) == 1 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     tc_fence_before();
@@ -1687,6 +1707,9 @@ template <int MODE>
 static LossLaunch loss_launch_of(bool list, int kind, bool pair) {
     if (kind == F32) return {loss_kernel_of<MODE, F32, false>(list), Shape<MODE, F32>::THREADS, Shape<MODE, F32>::A_PARTS, Shape<MODE, F32>::B_PARTS, 0};
     if (kind == BF16_FINE) return {loss_kernel_of<MODE, BF16_FINE, false>(list), Shape<MODE, BF16_FINE>::THREADS, Shape<MODE, BF16_FINE>::A_PARTS, 1, 0};
+    if constexpr (MODE != PRODUCTS)
+        if (kind == BF16_LONG)
+            return {pair ? loss_kernel_of<MODE, BF16_LONG, true>(list) : loss_kernel_of<MODE, BF16_LONG, false>(list), Shape<MODE, BF16_LONG>::THREADS, 1, 1, pair};
     return {pair ? loss_kernel_of<MODE, BF16, true>(list) : loss_kernel_of<MODE, BF16, false>(list), Shape<MODE, BF16>::THREADS, 1, 1, pair};
 }
 
@@ -1700,9 +1723,10 @@ static cudaError_t loss_set_attributes() {
     std::lock_guard<std::mutex> lock(g_loss_mutex);
     if (done_on[dev]) return cudaSuccess;
     for (int list = 0; list < 2; ++list)
-        for (int kind = 0; kind <= F32; ++kind)      // (0: bf16 in pairs)
-            for (const LossLaunch& l : {loss_launch_of<FORWARD>(list, kind, !kind), loss_launch_of<LOGITS>(list, kind, !kind), loss_launch_of<PRODUCTS>(list, kind, !kind)})
-                if ((e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + 1024)) != cudaSuccess) return e;
+        for (int kind = BF16; kind <= BF16_LONG; ++kind)
+            for (const bool pair : {false, true})
+                for (const LossLaunch& l : {loss_launch_of<FORWARD>(list, kind, pair), loss_launch_of<LOGITS>(list, kind, pair), loss_launch_of<PRODUCTS>(list, kind, pair)})
+                    if ((e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + 1024)) != cudaSuccess) return e;
     done_on[dev] = true;
     return cudaSuccess;
 }
@@ -1711,12 +1735,6 @@ static int vec_rows(const void* p, int64_t ld, int H, bool f32) {   // accesses 
     const uintptr_t at = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (f32 ? 4 : 2));
     return H % 8 || at % 16 ? 0 : at % 32 ? 1 : 2;
 }
-
-// Tensor cores cut what they add to an fp32 accumulator, so that a sum of n additions (16 products each) is short by a share of itself.
-// That share is put back as n 2^-26: measured over 4096 rows it is n times 2^-26 for normal operands and for ones that are correlated with
-// W, 0.5 to 0.6 of that where one of them has no negative values, 2 to 4 times it where neither has.  Logits of 2048 normal products are
-// 1.1e-6 off instead of 2.2e-6, of correlated ones 2.5e-7 instead of 2.1e-6.
-static float cut_share(int H) { return (float)(H / 16) * 1.4901161e-8f; }
 
 // (every kernel here waits for the one before it ahead of its first access to memory)
 template <typename... Params, typename... Args>
@@ -1834,7 +1852,6 @@ cudaError_t loss_run(const LossCall& c) {
     p.kb = L.Hp / BK;
     p.tn = L.tn;
     p.rtau = 1.f / c.tau;
-    p.whole = L.kind == BF16 ? 1.f + cut_share(L.Hp) : 1.f;
     p.bias = c.o.b;
     p.src = r.src; p.target = r.target_c; p.list = r.list; p.where = r.where; p.where_ld = r.where_ld;
     const int few = std::min(BM, up(c.N, 8));    // rows of A that a fetch brings
@@ -1843,6 +1860,7 @@ cudaError_t loss_run(const LossCall& c) {
     else e = loss_map(&map_x, r.xc, L.planes, L.Npad, L.Hp, L.Hp, few);
     if (e != cudaSuccess) return e;
     if ((e = loss_map(&map_w, w, L.planes, c.o.n_out, w_cols, ldw, L.pair ? L.tn / 2 : L.tn)) != cudaSuccess) return e;
+    const int logits_kind = L.kind == BF16 && p.kb > kLongBlocks ? BF16_LONG : L.kind;
     const int row_tiles = L.Npad / BM;
     const long long logit_rows = L.pair ? row_tiles / 2 : row_tiles;    // tiles
     if (!c.grad) {
@@ -1850,7 +1868,7 @@ cudaError_t loss_run(const LossCall& c) {
         p.pm = reinterpret_cast<float*>(c.ws + L.pm);
         p.ps = reinterpret_cast<float*>(c.ws + L.ps);
         p.pq = reinterpret_cast<float*>(c.ws + L.pq);
-        const LossLaunch l = loss_launch_of<FORWARD>(c.K > 0, L.kind, L.pair);
+        const LossLaunch l = loss_launch_of<FORWARD>(c.K > 0, logits_kind, L.pair);
         ring_of(p, l, few, L.tn);
         p.next = direct ? nullptr : r.next;
         if (direct) { p.direct = c.N; p.src = nullptr; p.target = c.target; }
@@ -1889,7 +1907,7 @@ cudaError_t loss_run(const LossCall& c) {
         p.n_vt = cdiv(p.cols, L.tn);
         p.add_dx = piece > 0;
         p.dbp = !c.db ? nullptr : one_tile ? c.db + p.v0 : reinterpret_cast<float*>(c.ws + L.dbp);
-        const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, L.kind, L.pair);
+        const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, logits_kind, L.pair);
         ring_of(p, l, few, L.tn);
         p.next = r.next + 2 * piece;
         if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_store, map_w, p, c.stream)) != cudaSuccess) return e;
