@@ -762,6 +762,9 @@ __device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {    // arrives at
                  "h"((uint16_t)3)
                  : "memory");
 }
+__device__ __forceinline__ void tc_commit_pair_here(uint64_t* bar) {    // arrives at this CTA's alone
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t ncols) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(ncols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -1193,7 +1196,9 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (!ok) break;
                 t = then;
             }
-            if (!ok && rank == 0) {   // given up: the copies in flight still write into shared memory (of both CTAs, which leave together)
+            // Copies in flight still write into shared memory (of both CTAs of a pair, which leave together): whoever gave up, and whenever, this
+            // thread stays until they are there, or another limit has run out.  (In a normal end there is nothing left to wait for.)
+            if (rank == 0) {
                 int late = 0;
                 for (int i = 0; i < p.stages; ++i) {
                     const uint32_t uses = turn + (i < s);        // of stage i
@@ -1249,12 +1254,11 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     }
                 }
             }
-            if (!ok || *reinterpret_cast<volatile int*>(&abort_flag)) {   // given up: the products in flight still read it
-                int late = 0;
-                if (PAIR) tc_commit_pair(&drain_bar);
-                else tc_commit(&drain_bar);
-                mbar_wait(&drain_bar, 0, &late);
-            }
+            // likewise the products in flight, which read shared memory and write tensor memory
+            int late = 0;
+            if (PAIR) tc_commit_pair_here(&drain_bar);
+            else tc_commit(&drain_bar);
+            mbar_wait(&drain_bar, 0, &late);
         }
     } else {
         const int q = warp & 3, group = (warp - 2) >> 2;   // tensor-memory lane quadrant; which columns of the tile
