@@ -325,8 +325,11 @@ wind_status_t wind_distill_loss_grad(const wind_output_t* o, const void* x, int6
                                      int32_t K, float tau, const float* lse, const float* dloss, void* dx, int64_t lddx, void* dw, int64_t lddw,
                                      float* db, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Waits for `stream` and returns the status of the last loss or gradient call that used `workspace`: WIND_OK, WIND_ERR_INVALID_ARG
- * (a target or id that is no label) or WIND_ERR_TIMEOUT. */
+/*
+ * Waits for `stream` and returns what the calls that used `workspace` found: WIND_ERR_TIMEOUT if a wait ran out in any of them since the
+ * workspace was last asked (what that call wrote, and what later ones made of it, is undefined; asking takes the mark back), else
+ * the status of the last loss or gradient call: WIND_OK or WIND_ERR_INVALID_ARG (a target or id that is no label).
+ */
 wind_status_t wind_loss_status(const void* workspace, void* stream);
 
 /*
@@ -515,6 +518,13 @@ wind_status_t wind_bench_joint(const wind_model_t* m, int32_t B, int32_t W, int3
  * mention of a safeguard is the beam-search footnote about not staying on one frame forever).
  */
 int32_t wind_debug_stall_barrier(int32_t extra_arrivals);
+
+/*
+ * The same for the losses of the output layer: in the calls that follow, one wait of the first CTA (or pair of CTAs) of one kernel asks
+ * for an arrival more than there will be.  which = 3 * kernel + wait: kernel 0 the loss's products, 1 the gradient's share of logits, 2 the
+ * products of dx and dW; wait 1 for operands, 2 for products, 3 for the next tile.  0 restores normal operation.  Returns the previous value.
+ */
+int32_t wind_debug_stall_loss(int32_t which);
 
 /*
  * Options of the tensor-core loop's tile planner, process-wide (defaults: 1, -1, 4, -1).  Meant for tests and

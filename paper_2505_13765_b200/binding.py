@@ -34,7 +34,7 @@ EXPORTS = [
     "wind_workspace_bytes", "wind_decode_greedy", "wind_decode_window_greedy", "wind_host_staging_bytes", "wind_decode_greedy_host",
     "wind_eval_joint_window", "wind_window_first_output", "wind_eval_joint_window_static", "wind_profile_decode", "wind_beam_workspace_bytes", "wind_beam_search", "wind_plan_batches", "wind_read_stats", "wind_set_trace", "wind_read_trace", "wind_debug_stall_barrier", "wind_set_kernels", "wind_status_string", "wind_last_cuda_error",
     "wind_set_loop_options", "wind_debug_plan", "wind_debug_cluster_smem", "wind_debug_beam_plan", "wind_bench_joint", "wind_refill_workspace_bytes", "wind_decode_greedy_refill", "wind_debug_loop_kernel",
-    "wind_loss_workspace_bytes", "wind_label_loss", "wind_label_loss_grad", "wind_distill_loss", "wind_distill_loss_grad", "wind_loss_status",
+    "wind_loss_workspace_bytes", "wind_label_loss", "wind_label_loss_grad", "wind_distill_loss", "wind_distill_loss_grad", "wind_loss_status", "wind_debug_stall_loss",
 ]
 
 _vp = C.c_void_p
@@ -156,6 +156,8 @@ def load_library():
     L.wind_read_trace.restype = i32
     L.wind_debug_stall_barrier.argtypes = [i32]
     L.wind_debug_stall_barrier.restype = i32
+    L.wind_debug_stall_loss.argtypes = [i32]
+    L.wind_debug_stall_loss.restype = i32
     L.wind_set_kernels.argtypes = [i32]
     L.wind_set_kernels.restype = i32
     L.wind_set_loop_options.argtypes = [i32, i32, i32, i32]
@@ -268,6 +270,11 @@ def wind_read_trace(model: "WindModel", B: int, T: int, W: int, workspace, strea
 def wind_debug_stall_barrier(extra_arrivals: int) -> int:
     """Test hook: make the loop kernel's grid barrier unfillable (see wind.h); 0 restores normal operation."""
     return load_library().wind_debug_stall_barrier(extra_arrivals)
+
+
+def wind_debug_stall_loss(which: int) -> int:
+    """Test hook: one wait of a kernel of the losses that cannot end (see wind.h); 0 restores normal operation."""
+    return load_library().wind_debug_stall_loss(which)
 
 
 def wind_set_kernels(kernels: int) -> int:
@@ -723,7 +730,7 @@ def wind_distill_loss_grad(x, weight, bias, ids, teacher, tau: float, lse, dloss
 
 
 def wind_loss_status(workspace, stream=None, check: bool = True) -> int:
-    """Waits for the stream; the status of the last loss or gradient call that used `workspace`."""
+    """Waits for the stream; WIND_ERR_TIMEOUT if a wait ran out in a call on `workspace` since it was last asked, else the last call's status."""
     torch = _ready()
     if stream is None:
         stream = torch.cuda.current_stream(workspace.device)

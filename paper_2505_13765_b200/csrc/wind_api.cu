@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -557,7 +558,11 @@ wind_status_t wind_loss_status(const void* workspace, void* stream) {
     LossCtrl h{};
     WIND_CUDA(cudaMemcpyAsync(&h, workspace, sizeof(h), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
     WIND_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
-    return (wind_status_t)h.status;
+    if (h.timed_out != kLossTimedOut) return (wind_status_t)h.status;
+    void* at = static_cast<uint8_t*>(const_cast<void*>(workspace)) + offsetof(LossCtrl, timed_out);
+    WIND_CUDA(cudaMemsetAsync(at, 0, sizeof(h.timed_out), (cudaStream_t)stream));
+    WIND_CUDA(cudaStreamSynchronize((cudaStream_t)stream));      // (a next call may be on another stream)
+    return WIND_ERR_TIMEOUT;
 }
 
 // Scratch of wind_eval_joint_window_static.  In host code `g_static_ws` is only a handle for
@@ -838,6 +843,8 @@ wind_status_t wind_bench_joint(const wind_model_t* m, int32_t B, int32_t W, int3
 }
 
 int32_t wind_debug_stall_barrier(int32_t extra_arrivals) { return loop_set_extra_arrivals(extra_arrivals); }
+
+int32_t wind_debug_stall_loss(int32_t which) { return loss_set_stall(which); }
 
 void wind_set_loop_options(int32_t resident, int32_t joint_placement, int32_t max_joint_waves, int32_t dataflow) {
     LoopOptions o;

@@ -38,12 +38,14 @@
 //                                            against 5200 of products), PRODUCTS 38, gathering 2 x 11.5 at 2.9 TB/s, joining and sums 11
 //     1 row, 1024, 8193 (loss)               12 us, floor 2.6: two launches, W read at 5 TB/s
 //
-// Every wait on an mbarrier is bounded: after about two seconds the CTA flags WIND_ERR_TIMEOUT, frees its tensor memory and returns.
+// Every wait on an mbarrier is bounded: after about two seconds the CTA marks the workspace as timed out, frees its tensor memory and returns.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <math_constants.h>
 
 #include <algorithm>
+#include <atomic>
+#include <cstddef>
 #include <mutex>
 
 #include "wind_internal.cuh"
@@ -526,6 +528,7 @@ struct LossGemm {
     int v0, cols, n_vt;           // this piece's first output, its outputs (to n_out at most) and tiles
     int32_t* next;                // units that were taken, beyond the CTAs' first ones; null: CTAs take them in turn
     int direct;                   // FORWARD: x as the caller has it, this many rows; 0: gathered rows
+    int stall;                    // test hook: the first CTA's or pair's wait that cannot end (1: operands, 2: products, 3: the next unit)
     float rtau;                   // 1 / tau
     const float* bias;
     const int32_t* src; const int32_t* target; const int2* list; const uint8_t* where; int where_ld;
@@ -1107,9 +1110,10 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int s = 0; s < p.stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], (PAIR ? 2 : 1) * EPI / 32); }
-        for (int i = 0; i < UNITS; ++i) { mbar_init(&units.full[i], 1); mbar_init(&units.empty[i], PAIR ? 4 : 2); }
+        auto arrivals = [&](int i, int what) { return 1u + (i == 0 && cta == 0 && p.stall == what); };
+        for (int s = 0; s < p.stages; ++s) { mbar_init(&full_bar[s], arrivals(s, 1)); mbar_init(&empty_bar[s], 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], arrivals(a, 2)); mbar_init(&acc_empty[a], (PAIR ? 2 : 1) * EPI / 32); }
+        for (int i = 0; i < UNITS; ++i) { mbar_init(&units.full[i], arrivals(i, 3)); mbar_init(&units.empty[i], PAIR ? 4 : 2); }
         mbar_init(&drain_bar, 1);
         fence_barrier_init();
         prefetch_tmap(&map_a); prefetch_tmap(&map_b);
@@ -1398,10 +1402,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         if (PAIR) tmem_dealloc_pair(tmem_base, 512);
         else tmem_dealloc(tmem_base, 512);
     }
-    if (threadIdx.x == 0) {
-        if (MODE == FORWARD && p.direct) p.ctrl->gave_up[blockIdx.x] = abort_flag;      // (nobody has set the status of this call yet)
-        else if (abort_flag) atomicCAS(&p.ctrl->status, 0, (int)WIND_ERR_TIMEOUT);
-    }
+    if (threadIdx.x == 0 && abort_flag) p.ctrl->timed_out = kLossTimedOut;
 }
 
 // ---------------------------------------------------------------------------
@@ -1415,7 +1416,7 @@ struct CombineParams {
     int parts, Npad;
     const float* ent; float tau;
     float *loss, *lse;
-    int direct, ctas, n_out; const int32_t* target; const uint8_t* mark;   // direct: rows were not gathered; what they are stands in target or mark
+    int direct, n_out; const int32_t* target; const uint8_t* mark;   // direct: rows were not gathered; what they are stands in target or mark
 };
 
 __global__ void __launch_bounds__(256) loss_combine_kernel(const CombineParams p) {
@@ -1426,8 +1427,7 @@ __global__ void __launch_bounds__(256) loss_combine_kernel(const CombineParams p
     const int j = blockIdx.x * 8 + at_row, n = p.direct ? p.direct : p.ctrl->n_rows;
     if (p.direct && blockIdx.x == 0) {
         const bool bad = __syncthreads_or((int)threadIdx.x < n && mark_of(p.target, p.mark, p.n_out, threadIdx.x) == ROW_BAD);
-        const bool late = __syncthreads_or((int)threadIdx.x < p.ctas && p.ctrl->gave_up[threadIdx.x]);
-        if (threadIdx.x == 0) { p.ctrl->status = bad ? WIND_ERR_INVALID_ARG : late ? WIND_ERR_TIMEOUT : WIND_OK; p.ctrl->n_rows = n; }
+        if (threadIdx.x == 0) { p.ctrl->status = bad ? WIND_ERR_INVALID_ARG : WIND_OK; p.ctrl->n_rows = n; }
     }
     if ((int)blockIdx.x * 8 >= n) return;
     const float *pm = p.pm, *ps = p.ps, *pq = p.pq;
@@ -1777,6 +1777,13 @@ static cudaError_t launch_gemm(const LossLaunch& l, long long units, int sms, co
     return cudaLaunchKernelExC(&cfg, (const void*)l.kernel, args);
 }
 
+static std::atomic<int> g_loss_stall{0};   // 0, or 3 x kernel + wait
+int loss_set_stall(int which) { return g_loss_stall.exchange(which >= 1 && which <= 9 ? which : 0); }
+static int stall_of(LossMode mode) {
+    const int which = g_loss_stall.load() - 3 * mode;
+    return which >= 1 && which <= 3 ? which : 0;
+}
+
 cudaError_t loss_run(const LossCall& c) {
     const LossLayout& L = c.lay;
     const bool f32 = c.o.dtype == WIND_DT_F32;
@@ -1788,7 +1795,7 @@ cudaError_t loss_run(const LossCall& c) {
     if (e != cudaSuccess) return e;
     LossCtrl* ctrl = reinterpret_cast<LossCtrl*>(c.ws + L.ctrl);
     if (c.N == 0) {   // no rows: no loss, no gradient
-        e = cudaMemsetAsync(ctrl, 0, sizeof(LossCtrl), c.stream);
+        e = cudaMemsetAsync(ctrl, 0, offsetof(LossCtrl, timed_out), c.stream);
         if (e == cudaSuccess && c.grad && c.dw) e = cudaMemset2DAsync(c.dw, (size_t)c.lddw * es, 0, (size_t)c.o.H * es, (size_t)c.o.n_out, c.stream);
         if (e == cudaSuccess && c.grad && c.db) e = cudaMemsetAsync(c.db, 0, 4 * (size_t)c.o.n_out, c.stream);
         return e;
@@ -1797,7 +1804,6 @@ cudaError_t loss_run(const LossCall& c) {
     if ((e = loss_set_attributes()) != cudaSuccess) return e;
     int sms = 0;
     if ((e = loop_sm_count(&sms)) != cudaSuccess) return e;
-    sms = std::min(sms, kLossMaxCtas);
 
     RowsParams r{};
     r.ctrl = ctrl;
@@ -1878,12 +1884,13 @@ cudaError_t loss_run(const LossCall& c) {
         if (direct) { p.direct = c.N; p.src = nullptr; p.target = c.target; }
         const bool final = !direct && L.parts == 1;     // (no launch for joining what is one part)
         if (final) { p.loss = c.loss; p.lse = c.lse_out; p.ent = c.K ? r.ent : nullptr; p.tau = c.tau; }
+        p.stall = stall_of(FORWARD);
         if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_x, map_w, p, c.stream)) != cudaSuccess) return e;
         if (final) return cudaSuccess;
         CombineParams q{};
         q.ctrl = ctrl; q.src = r.src; q.pm = p.pm; q.ps = p.ps; q.pq = p.pq; q.parts = L.parts; q.Npad = L.Npad;
         q.ent = c.K ? r.ent : nullptr; q.tau = c.tau; q.loss = c.loss; q.lse = c.lse_out;
-        q.direct = p.direct; q.ctas = (int)std::min<long long>((long long)row_tiles * p.n_vt, sms); q.n_out = c.o.n_out; q.target = c.target; q.mark = c.K ? r.mark : nullptr;
+        q.direct = p.direct; q.n_out = c.o.n_out; q.target = c.target; q.mark = c.K ? r.mark : nullptr;
         return launch_small(loss_combine_kernel, cdiv(c.N, 8), c.stream, q);
     }
 
@@ -1914,6 +1921,7 @@ cudaError_t loss_run(const LossCall& c) {
         const LossLaunch l = loss_launch_of<LOGITS>(c.K > 0, logits_kind, L.pair);
         ring_of(p, l, few, L.tn);
         p.next = r.next + 2 * piece;
+        p.stall = stall_of(LOGITS);
         if ((e = launch_gemm(l, logit_rows * p.n_vt, sms, map_x, map_w, map_store, map_w, p, c.stream)) != cudaSuccess) return e;
         FinishParams f{};
         f.ctrl = ctrl; f.H = c.o.H; f.Hp = L.Hp; f.cols = p.cols;
@@ -1929,6 +1937,7 @@ cudaError_t loss_run(const LossCall& c) {
         const int tm = lp.pair ? 2 * BM : BM;
         const long long units = (c.dx ? (long long)L.s_dx * (L.Npad / tm) * p.ht : 0) + (c.dw ? (long long)L.s_dw * cdiv(p.cols, tm) * p.ht : 0);
         p.next = r.next + 2 * piece + 1;
+        p.stall = stall_of(PRODUCTS);
         if (units && (e = launch_gemm(lp, units, sms, map_g, map_w64, map_g64, map_x64, p, c.stream)) != cudaSuccess) return e;
         if (c.dw && L.slab_dw) {
             f.sdw = p.sdw; f.s_dw = L.s_dw; f.slab_rows_dw = p.slab_rows_dw;

@@ -9,7 +9,6 @@
 namespace wind {
 
 constexpr int kLossMaxK = 256;            // teacher's entries of a row
-constexpr int kLossMaxCtas = 256;
 constexpr long long kLossMaxLogits = 1ll << 40;   // N n_out
 constexpr int kLossMaxRows = 1 << 24;
 constexpr int kLossMaxOut = (1 << 24) - 1;
@@ -18,10 +17,13 @@ constexpr size_t kLossPieceBytes = (size_t)512 << 20;   // the gradient's share 
 
 // Control words, first thing in the workspace.
 struct LossCtrl {
-    int32_t status;   // wind_status_t, first error wins
+    int32_t status;   // of the last call: WIND_OK or WIND_ERR_INVALID_ARG
     int32_t n_rows;   // rows with a loss
-    int32_t gave_up[kLossMaxCtas];   // CTAs whose waits ran out, where nothing runs ahead of them that could reset `status`
+    // kLossTimedOut: a wait ran out, in this call or in an earlier one.  Only wind_loss_status takes it back: a gradient that reads what a
+    // timed-out loss wrote is as wrong as that.  (64 bits: a workspace nobody has written yet should not say so by chance.)
+    unsigned long long timed_out;
 };
+constexpr unsigned long long kLossTimedOut = 0x9c0e5d2b71f6a843ull;
 
 // How a call is cut up, and the byte offsets of its workspace regions.  Host arithmetic on the sizes alone.
 struct LossLayout {
@@ -58,5 +60,6 @@ struct LossCall {
 // most_of_fewer: `total` is the most that a call of up to N rows needs (the offsets are not to be used).
 LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most_of_fewer = false);
 cudaError_t loss_run(const LossCall& c);
+int loss_set_stall(int which);   // test hook (wind_debug_stall_loss); the previous value
 
 }  // namespace wind
