@@ -1283,7 +1283,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             // what the row needs besides its logits, under way while these are made
             const bool there = row < n_rows;
             const int col = p.v0 + t.nt * p.tn + my0;
-            Targets<LIST> targets(p, row, MODE != PRODUCTS && there && my0 < p.tn, col);
+            Targets<LIST> targets(p, row, MODE != PRODUCTS && there && my0 < p.tn && col < p.n_out, col);   // (behind the outputs: nothing to find, and no `where`)
             const float scale = MODE == LOGITS && there ? p.scale[row] : 0.f, nlse = MODE == LOGITS && there ? p.nlse[row] : 0.f;
             if (MODE != PRODUCTS && et < p.tn) {
                 const int v = p.v0 + t.nt * p.tn + et;         // outputs behind the last one: probability zero
