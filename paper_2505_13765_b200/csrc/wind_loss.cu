@@ -63,7 +63,8 @@ constexpr int LT_BAND = 16;               // row tiles that are worked on togeth
 constexpr int ROWS_COUNTED = 32768;       // longer calls have the rows that count counted by a kernel of its own, so many at a time
 constexpr int PANEL_BYTES = 64 * BK * 2;  // 64 x 64 bf16
 constexpr int kFillCtas = 148;            // CTAs that a product is cut for
-constexpr int kNarrowTiles = 4 * kFillCtas;   // so many tiles or more are not made narrower, nor their sums cut
+constexpr int kNarrowTiles = 4 * kFillCtas;   // so many tiles or more are not made narrower, nor their sums cut to fill the chip
+constexpr int kSumAdditions = 4096;       // of an accumulator of dx and dW: at most 4096 x 2^-23 = 2^-11 is lost, of results rounded to 2^-8
 
 static inline int up(long long a, int b) { return (int)((a + b - 1) / b * b); }
 static inline int cdiv(long long a, int b) { return (int)((a + b - 1) / b); }
@@ -1615,9 +1616,13 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
         // Parts of a sum: units of at most two thirds of a CTA's share of all K blocks, so that the units taken last fill the gaps, but of
         // 8 K blocks (bf16) at least, and none where the tiles alone are many.
         const int least_kb = cdiv(8, terms);
+        // And of at most so many that a bf16 sum stays below kSumAdditions: the tensor cores cut, all one way (2^21 rows of positive
+        // activations in one accumulator: dW 1e-3 short).  (fp32 adds each K block up in registers.)
+        const int most_kb = f32 ? 1 << 30 : kSumAdditions / (BK / 16) / L.kind;      // (a K block of the FINE kind is two terms long)
         const long long work = t_dx * kb_dx + t_dw * kb_dw, share = (2 * work + 3 * kFillCtas - 1) / (3 * kFillCtas);
         auto parts_of = [&](long long tiles, int kb) {
-            return tiles >= kNarrowTiles ? 1 : std::max(1, cdiv(kb, (int)std::min<long long>(std::max<long long>(share, least_kb), std::max(1, kb))));
+            const int fill = tiles >= kNarrowTiles ? 1 : cdiv(kb, (int)std::min<long long>(std::max<long long>(share, least_kb), std::max(1, kb)));
+            return std::max({1, fill, cdiv(kb, most_kb)});
         };
         L.s_dx = parts_of(t_dx, kb_dx);
         L.s_dw = parts_of(t_dw, kb_dw);
@@ -1633,6 +1638,13 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
             const long long all_dw = (long long)cdiv(o.n_out, 128) * ht;
             sdx = slab(L.pieces > 1 ? t_dx : std::min<long long>(t_dx, kNarrowTiles), kb_dx);
             sdw = slab(std::min<long long>(all_dw, kNarrowTiles), kb_dw);
+            if (!f32) {
+                // sums cut for their length: parts x rows of dW's slab, where a piece is 2048 outputs or as many as keep g within its limit
+                // (4096 at the 65536 rows from which on there are parts), and parts x rows of dx's, where a piece is above 32768 outputs
+                const size_t p_dw = cdiv(L.Npad / BK, most_kb), p_dx = cdiv(cdiv(o.n_out, BK), most_kb / 2);
+                if (p_dw > 1) sdw = std::max(sdw, std::min(p_dw * up(o.n_out, 128), std::max<size_t>(p_dw * 2048, 8192)) * L.Hp);
+                if (p_dx > 1) sdx = std::max(sdx, std::min<size_t>(p_dx * np, 8192) * L.Hp);
+            }
             const size_t whole = np * (size_t)all, limit = kLossPieceBytes / 2;
             g = std::min((size_t)L.planes * whole, std::max(limit, (size_t)L.planes * np * 2048));
             if (!f32) g = std::max(g, std::min<size_t>(2 * std::min(np, (size_t)256) * all, std::max(limit, 2 * std::min(np, (size_t)256) * 2048)));

@@ -60,3 +60,43 @@ def test_long_sums_of_logits(pkg, N, H, V, kind):  # noqa: F811
     if kind == "normal" and H > 1024:
         share = float(((got - want) * want.sign()).sum() / want.abs().sum())
         assert abs(share) <= 64 * 2.0 ** -25, share
+
+
+def test_long_sums_of_dw(pkg):  # noqa: F811
+    """Two million rows of positive activations against equal probabilities: dW's sums are cut one way, but only within an accumulator."""
+    N, H, V = 1 << 21, 1792, 2048
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = (0.5 + 0.5 * torch.rand(N, H, generator=g, device=DEV, dtype=torch.bfloat16)).clamp_(max=1.0)
+    w = torch.zeros(V, H, dtype=torch.bfloat16, device=DEV)
+    t = torch.zeros(N, dtype=torch.int32, device=DEV)
+    lse = torch.full((N,), math.log(V), device=DEV)
+    dw = torch.full((V, H), math.nan, dtype=torch.bfloat16, device=DEV)
+    ws = pkg.alloc_loss_workspace(w, N, 0, True)
+    pkg.wind_label_loss_grad(x, w, None, t, lse, None, None, dw, None, ws, check=True)
+    # g is 2^-11 but for the target's output (of which lse's rounding, at most 2^-21 relative, is lost in g's rounding to bf16)
+    want = torch.stack([x[:, h0: h0 + 128].sum(0, dtype=torch.float64) for h0 in range(0, H, 128)]).flatten() * 2.0 ** -11
+    # The columns' sums are 767 with a sigma of 0.1, bf16's step there is 4: all round the same way, by up to half a step, so that neither a
+    # column's nor the mean's distance says anything below 2^-8.  Rounding is monotone, though: the fp32 sum lies between the exact one less
+    # 4096 cuts of at most 2^-23 of the accumulator (half its end on the mean, as it grows evenly) and the exact one plus 32 joinings' 2^-24.
+    low, high = ((want * f).float().bfloat16() for f in (1.0 - 4096 * 2.0 ** -24, 1.0 + 32 * 2.0 ** -24))
+    assert bool((dw[1:] >= low).all()) and bool((dw[1:] <= high).all()), (float(dw[1:].min()), float(dw[1:].max()), float(low.min()), float(high.max()))
+
+
+@pytest.mark.parametrize("N,H,V,kinds", [(70000, 264, 1100, ("dx", "dw", "db")), (131100, 1544, 300, ("dw",)), (200, 136, 70001, ("dx", "dw", "db"))])
+def test_sums_cut_for_their_length(pkg, N, H, V, kinds):  # noqa: F811
+    """Rows and outputs from which on a sum of dW or dx has several parts for its length, ragged ones among them."""
+    from test_gpu_loss import verify_in_slices
+    c = make(N + H, "bf16", N, H, V, pad=0.1)
+    got = call(pkg, c, want=kinds)
+    if len(kinds) == 3:
+        verify_in_slices(got, c, 20000)
+        return
+    keep = c["t"] >= 0
+    z = torch.where(keep[:, None], c["x"].float(), 0.0).double() @ c["w"].double().T + c["b"].double()
+    q = torch.exp(z - torch.logsumexp(z, 1, keepdim=True))
+    q[torch.arange(N, device=DEV)[keep], c["t"][keep].long()] -= 1.0
+    q *= torch.where(keep, c["dloss"].double(), 0.0)[:, None]
+    xd = torch.where(keep[:, None], c["x"].double(), 0.0)
+    want, size = q.T @ xd, q.abs().T @ xd.abs()
+    # a bf16 rounding of g and one of dW, the sums' cuts, and what p is off (a share of g of at most 2^-10: logits 2^-14 off)
+    assert bool(((got["dw"].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -10 + 2.0 ** -11) * size + 2.0 ** -8 * want.abs()).all())
