@@ -312,7 +312,7 @@ wind_status_t wind_label_loss_grad(const wind_output_t* o, const void* x, int64_
                                    size_t workspace_bytes, void* stream);
 
 /*
- * The same against a teacher's K best labels, 1 <= K <= WIND_LOSS_MAX_ENTRIES, 0 < tau < inf (lse: of z / tau).
+ * The same against a teacher's K best labels, 1 <= K <= WIND_LOSS_MAX_ENTRIES, FLT_MIN <= tau < inf (lse: of z / tau).
  *   ids      [N, K] int32 in [0, n_out) in any order, or -1: the teacher has no such entry (wind_window_first_output writes its lists so).
  *            A label that stands there twice counts with both entries.
  *   teacher  [N, K] fp32 logits or natural-log probabilities; -inf: probability 0.  Not read where ids is -1.

@@ -3,6 +3,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstddef>
 #include <cstdio>
@@ -497,7 +498,8 @@ static wind_status_t enqueue_loss(LossCall& c, const wind_output_t* o, const voi
                                   size_t workspace_bytes, void* stream) {
     wind_status_t s = check_output(o, N, K);
     if (s != WIND_OK) return s;
-    if (!o->w || !workspace || ldx < 0 || !(tau > 0.f) || !(tau < INFINITY)) return WIND_ERR_INVALID_ARG;
+    // (of a tau below the normal numbers the kernels would make an infinite 1 / tau)
+    if (!o->w || !workspace || ldx < 0 || !(tau >= FLT_MIN) || !(tau < INFINITY)) return WIND_ERR_INVALID_ARG;
     if (N > 0 && !x) return WIND_ERR_INVALID_ARG;
     if (c.grad && ((c.dx && c.lddx < o->H) || (c.dw && c.lddw < o->H))) return WIND_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) % kAlign) return WIND_ERR_WORKSPACE;

@@ -35,3 +35,12 @@ def test_reported_sizes_are_enough_over_the_whole_range(lib):  # noqa: F811
             st = f(ref, p, H, *rows, p, p, p, H, p, H, p, ws, have, None)
             assert st == bd.WIND_ERR_CUDA, (st, H, n_out, o.dtype, N, n, K)
     assert n_long > 500
+
+
+def test_temperatures_without_a_reciprocal_are_refused(lib):  # noqa: F811
+    o, p, ws = C.byref(layer()), 1 << 20, 1 << 21
+    for tau in (1e-45, 1e-39, 3e-39, 1.17e-38):
+        assert lib.wind_distill_loss(o, p, 640, p, p, 4, 8, tau, p, p, ws, 1 << 40, None) == bd.WIND_ERR_INVALID_ARG
+        assert lib.wind_distill_loss_grad(o, p, 640, p, p, 4, 8, tau, p, p, p, 640, p, 640, p, ws, 1 << 40, None) == bd.WIND_ERR_INVALID_ARG
+    for tau in (2.0 ** -126, 3e38):      # (refused for the workspace alone)
+        assert lib.wind_distill_loss(o, p, 640, p, p, 4, 8, tau, p, p, ws, 100, None) == bd.WIND_ERR_WORKSPACE
