@@ -510,8 +510,9 @@ static wind_status_t enqueue_loss(LossCall& c, const wind_output_t* o, const voi
                             reinterpret_cast<uintptr_t>(c.lse) | reinterpret_cast<uintptr_t>(c.dloss) | reinterpret_cast<uintptr_t>(c.db);
     if (of_model % (o->dtype == WIND_DT_F32 ? 4 : 2) || words % 4) return WIND_ERR_INVALID_ARG;
     c.o = *o;
+    if (o->n_out == 1) c.o.ldw = o->H;      // (one row: whatever the distance says, tensor maps need a sensible one)
     c.x = x; c.ldx = ldx; c.N = N; c.K = K; c.tau = tau;
-    c.lay = loss_layout(*o, N, K, c.grad);
+    c.lay = loss_layout(c.o, N, K, c.grad);
     if (workspace_bytes < c.lay.total) return WIND_ERR_WORKSPACE;
     c.ws = static_cast<uint8_t*>(workspace);
     c.stream = (cudaStream_t)stream;

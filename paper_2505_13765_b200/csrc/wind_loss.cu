@@ -1567,7 +1567,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
     L.planes = f32 ? 3 : 1;
     L.kind = f32 ? F32 : N <= kFineRows ? BF16_FINE : BF16;
     L.g_planes = L.kind;
-    L.pack_w = f32 || o.H % 8 || o.ldw % 8 || (o.n_out > 1 && o.ldw < o.H) || reinterpret_cast<uintptr_t>(o.w) % 16;
+    L.pack_w = f32 || o.H % 8 || (o.n_out > 1 && (o.ldw % 8 || o.ldw < o.H)) || reinterpret_cast<uintptr_t>(o.w) % 16;
     L.Hp = up(o.H, 64);
     L.Npad = N <= BM ? up(N, BM) : up(N, 2 * BM);
     size_t off = 0;
