@@ -545,8 +545,13 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
+def _tensor(t, name: str) -> None:
+    _need(hasattr(t, "data_ptr"), f"{name}: {'not given' if t is None else 'not a tensor'}")
+
+
 def _rows(t, name: str, shape, dtype, device) -> int:
     """Checks a matrix whose rows are contiguous; the distance between rows, in elements."""
+    _tensor(t, name)
     _need(t.dim() == 2 and tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
     _need(t.dtype == dtype and t.device == device, f"{name}: {t.dtype} on {t.device}, not {dtype} on {device}")
     _need(shape[1] == 1 or t.numel() == 0 or t.stride(1) == 1, f"{name}: the values of a row have to be contiguous")
@@ -557,6 +562,7 @@ def _vector(t, name: str, shape, dtype, device) -> int:
     """Checks a contiguous array; its address, 0 for None."""
     if t is None:
         return 0
+    _tensor(t, name)
     _need(tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
     _need(t.dtype == dtype and t.device == device, f"{name}: {t.dtype} on {t.device}, not {dtype} on {device}")
     _need(t.is_contiguous(), f"{name} has to be contiguous")
@@ -565,6 +571,7 @@ def _vector(t, name: str, shape, dtype, device) -> int:
 
 def _output_layer(weight, bias=None) -> wind_output_t:
     import torch
+    _tensor(weight, "weight")
     _need(weight.dim() == 2 and weight.dtype in (torch.bfloat16, torch.float32), "weight: a matrix [n_out, H], bf16 or fp32")
     n_out, H = weight.shape
     ldw = _rows(weight, "weight", (n_out, H), weight.dtype, weight.device)
@@ -609,6 +616,7 @@ def _check_loss_call(x, weight, bias, rows, forward, backward, workspace, stream
     dev, dt = weight.device, weight.dtype
     _need(dev.type == "cuda", "weight: on a CUDA device")
     n_out, H = weight.shape
+    _tensor(x, "x")
     _need(x.dim() == 2, "x: a matrix [N, H]")
     N = x.shape[0]
     _rows(x, "x", (N, H), dt, dev)
@@ -618,6 +626,7 @@ def _check_loss_call(x, weight, bias, rows, forward, backward, workspace, stream
     if len(rows) == 1:
         _vector(rows[0], "target", (N,), i32, dev)
     else:
+        _tensor(rows[0], "ids")
         _need(rows[0].dim() == 2, "ids: a matrix [N, K]")
         K = rows[0].shape[1]
         _vector(rows[0], "ids", (N, K), i32, dev)
@@ -634,6 +643,7 @@ def _check_loss_call(x, weight, bias, rows, forward, backward, workspace, stream
         if dw is not None:
             _rows(dw, "dw", (n_out, H), dt, dev)
         _vector(db, "db", (n_out,), f32, dev)
+    _tensor(workspace, "workspace")
     _need(workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace: contiguous bytes")
     _need(workspace.device == dev, f"workspace: on {workspace.device}, not {dev}")
     _need(stream is None or stream.device == dev, f"stream: not on {dev}")
@@ -661,8 +671,9 @@ def _vector_arg(t, shape, dtype, dev: int):
 def _loss_call(name: str, x, weight, bias, rows, forward, backward, workspace, stream, check: bool) -> int:
     """rows: (target,) or (ids, teacher, tau); forward: (loss, lse) or None; backward: (lse, dloss, dx, dw, db) or None."""
     torch = _torch_ready or _ready()
-    f32, i32, dt, dev = torch.float32, torch.int32, weight.dtype, weight.get_device()
+    f32, i32 = torch.float32, torch.int32
     try:
+        dt, dev = weight.dtype, weight.get_device()
         if dev < 0 or not (dt is torch.bfloat16 or dt is f32):
             raise _Unlike
         (n_out, H), (N, _) = weight.shape, x.shape

@@ -35,3 +35,25 @@ def test_a_single_row_may_be_any_distance_from_the_next(pkg, dtype, N):  # noqa:
                                         db.data_ptr(), ws.data_ptr(), size, stream) == 0
         assert lib.wind_loss_status(ws.data_ptr(), stream) == 0
         verify(dict(loss=loss, lse=lse, dx=dx, dw=dw, db=db), ref, ld)
+
+
+def test_what_is_no_tensor_is_refused_by_name(pkg):  # noqa: F811
+    c, d = make(1, "bf16", 6, 16, 9), make(2, "bf16", 6, 16, 9, 2)
+    ws = pkg.alloc_loss_workspace(c["w"], 6, 2, True)
+    v = [torch.empty(6, device=DEV) for _ in range(2)]
+    label = dict(x=c["x"], weight=c["w"], bias=c["b"], target=c["t"], loss=v[0], lse=v[1], workspace=ws)
+    distill = dict(x=d["x"], weight=d["w"], bias=d["b"], ids=d["ids"], teacher=d["y"], tau=1.0, loss=v[0], lse=v[1], workspace=ws)
+    grads = dict(dloss=None, dx=torch.empty_like(c["x"]), dw=torch.empty_like(c["w"]), db=torch.empty(9, device=DEV))
+    label_grad = {**{k: v for k, v in label.items() if k != "loss"}, **grads}
+    distill_grad = {**{k: v for k, v in distill.items() if k != "loss"}, **grads}
+    optional = ("bias", "dloss", "dx", "dw", "db", "tau")
+    for f, good in ((pkg.wind_label_loss, label), (pkg.wind_distill_loss, distill), (pkg.wind_label_loss_grad, label_grad),
+                    (pkg.wind_distill_loss_grad, distill_grad)):
+        f(**good, check=True)
+        for k in good:
+            for bad in ([1.0, 2.0], 3) + ((None,) if k not in optional else ()):
+                if k != "tau":
+                    with pytest.raises(ValueError, match=k if k not in ("loss", "lse") or bad is not None else "loss"):
+                        f(**{**good, k: bad})
+    with pytest.raises(ValueError, match="weight"):
+        pkg.alloc_loss_workspace(None, 6)
