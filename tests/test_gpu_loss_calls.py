@@ -57,3 +57,90 @@ def test_what_is_no_tensor_is_refused_by_name(pkg):  # noqa: F811
                         f(**{**good, k: bad})
     with pytest.raises(ValueError, match="weight"):
         pkg.alloc_loss_workspace(None, 6)
+
+
+WANTS = [("dx",), ("dw",), ("db",), ("dx", "db"), ("dw", "db"), ("dx", "dw")]
+
+
+@pytest.mark.parametrize("dtype,N,H,V,K,slices", [
+    ("bf16", 3000, 1024, 9001, 0, 0),         # a CTA to a tile of logits, two to one of dx and dW
+    ("bf16", 3000, 1208, 9001, 5, 0),         # the same with logits from several accumulators
+    ("bf16", 8192, 1544, 40000, 0, 2048),     # two pieces of the outputs, tiles by two CTAs throughout
+    ("bf16", 9000, 2048, 31000, 3, 1500),     # the last piece a fraction of the first, rows that end inside a tile
+    ("f32", 333, 136, 1100, 3, 0), ("bf16", 100, 64, 300, 0, 0), ("bf16", 7, 640, 1025, 8, 0), ("f32", 44001, 16, 2300, 0, 20000),
+    ("bf16", 140001, 24, 4200, 0, 20000),
+])
+def test_some_of_the_gradients_in_every_form(pkg, dtype, N, H, V, K, slices):  # noqa: F811
+    """All gradients against the definition, then any of them alone: the same bits, whatever else is asked for."""
+    c = make(N + H + V + K, dtype, N, H, V, K, pad=0.1 if N > 10 else 0.0)
+    got = call(pkg, c)
+    if slices:
+        verify_in_slices(got, c, slices)
+    else:
+        verify(got, reference(c))
+    for want in WANTS:
+        some = call(pkg, c, want=want)
+        for k in want:
+            assert torch.equal(some[k], got[k]), (want, k)
+
+
+@pytest.mark.parametrize("dtype,N,H,V,K", [("bf16", 900, 2048, 12289, 5), ("bf16", 3000, 1208, 9001, 0), ("f32", 500, 72, 700, 3), ("bf16", 70, 64, 300, 0)])
+def test_every_form_captured_and_replayed(pkg, dtype, N, H, V, K):  # noqa: F811
+    first, second = (make(s, dtype, N, H, V, K, pad=0.1) for s in (5, 6))
+    c = {k: (v.clone() if torch.is_tensor(v) else v) for k, v in first.items()}
+    ws = pkg.alloc_loss_workspace(c["w"], N, K, True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(pkg, c, ws=ws)
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = call(pkg, c, ws=ws, check=False)
+    for d in (second, first):
+        for k, v in d.items():
+            if torch.is_tensor(v):
+                c[k].copy_(v)
+        for v in out.values():
+            v.fill_(math.nan)
+        g.replay()
+        assert pkg.wind_loss_status(ws) == 0
+        verify(out, reference(d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_teacher_by_its_own_window_and_a_students_loss(pkg, dtype):  # noqa: F811
+    """The chain as a user runs it: the teacher's K best labels of single frames by wind_window_first_output go into the distillation of
+    another model's output layer as they are; an utterance without a frame there is a row of padding."""
+    import numpy as np
+    from naive_model import random_weights
+    r = np.random.default_rng(9)
+    B, T, V, K, H = 40, 12, 60, 7, 48
+    teacher = random_weights(r, 32, 64, 64, 2, 96, V, act=0, bias_scale=0.1)
+    enc = r.standard_normal((B, T, 32)).astype(np.float32)
+    lens = r.integers(1, T + 1, B).astype(np.int32)
+    lens[[3, 17]] = 0
+    t0 = np.where(lens > 0, r.integers(0, 100, B) % np.maximum(lens, 1), 0).astype(np.int32)
+    m = pkg.WindModel(teacher)
+    up = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    logp = torch.full((B, 1, V + 1), math.nan, device=DEV)
+    ids, jump = (torch.full((B, K), -7, dtype=torch.int32, device=DEV) for _ in range(2))
+    best = torch.full((B, K), math.nan, device=DEV)
+    pkg.wind_window_first_output(m, pkg.to_device_enc(m, enc), up(lens), 1, up(r.integers(0, V, (B, 3)).astype(np.int32)),
+                                 up(r.integers(0, 4, B).astype(np.int32)), up(t0), logp, pkg.alloc_workspace(m, B, T, 1), K=K, top_label=ids,
+                                 top_jump=jump, top_logp=best)
+    c = make(4, dtype, B, H, V + 1, pad=0.0)
+    del c["t"]
+    c.update(ids=ids, y=best, tau=2.0)
+    ref = reference(c)
+    assert ref["keep"].tolist() == [bool(n) for n in lens]
+    got = call(pkg, c)
+    verify(got, ref)
+    # and from the whole distribution that the teacher gave, with the same labels kept: log-probabilities, renormalised at tau
+    kept = torch.full((B, V + 1), -math.inf, dtype=torch.float64, device=DEV)
+    rows = ref["keep"]
+    kept[rows] = kept[rows].scatter(1, ids[rows].long(), logp[rows, 0].double().gather(1, ids[rows].long()))
+    q = torch.softmax(kept[rows] / 2, 1)
+    z = (c["x"].double() @ c["w"].double().T + c["b"].double())[rows] / 2
+    want = 4 * (torch.special.xlogy(q, q) - q * torch.log_softmax(z, 1)).sum(1)
+    assert bool(((got["loss"][rows].double() - want).abs() <= ref["tol_loss"]).all())
