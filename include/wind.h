@@ -260,8 +260,10 @@ wind_status_t wind_window_first_output(const wind_model_t* m, const void* enc, c
  * on: the first one loads the kernels): wind_loss_status waits and returns what the device found.
  *
  * Arithmetic: logits, exponentials, sums, lse, loss and db in fp32.  bf16 models: products of bf16 operands, g rounded to bf16 (to two
- * bf16 parts, 16 bits, in calls of up to 256 rows), dx and dW rounded to bf16 once.  fp32 models: every operand as the sum of three bf16
- * parts, and the part products above 2^-24 of a product, on the tensor cores; an infinite operand gives NaN there where fp32
+ * bf16 parts, 16 bits, in calls of up to 256 rows), dx and dW rounded to bf16 once.  Sums of products are made on the tensor cores, 16 products
+ * an addition, which cuts instead of rounding: by at most 2^-23 of the accumulator, all one way.  An accumulator takes at most 64 additions
+ * of a logit (4 up to 256 rows) and 4096 of dx and dW; accumulators are added up in fp32.  fp32 models: every operand as the sum of three bf16
+ * parts, and the part products above 2^-24 of a product, on the tensor cores, 24 additions an accumulator; an infinite operand gives NaN there where fp32
  * arithmetic gives an infinity.
  */
 typedef struct {
@@ -286,7 +288,8 @@ wind_status_t wind_loss_workspace_bytes(const wind_output_t* o, int32_t N, int32
 /*
  * Loss and log-sum-exp (of z / tau) of N rows against labels.
  *   x       [N, H], rows ldx elements apart (any distance, any address that is one of an element; 0: the same row)
- *   target  [N] int32 in [0, n_out), or -1: a row of padding.  Its loss and lse are 0 and its x is not read (it may hold NaN).
+ *   target  [N] int32 in [0, n_out), or -1: a row of padding.  Its loss and lse are 0, whatever its x holds (NaN, say); it may be
+ *           read all the same.
  *           With another value loss and lse of that row are NaN, no output is read through it and the status is WIND_ERR_INVALID_ARG.
  *   loss, lse  [N] fp32
  *   workspace  device memory, 256-byte aligned, at least wind_loss_workspace_bytes(o, N, 0, 0).  Calls sharing a workspace must not
@@ -304,7 +307,8 @@ wind_status_t wind_label_loss(const wind_output_t* o, const void* x, int64_t ldx
  *   dx      [N, H] of the model's dtype, rows lddx >= H elements apart, or NULL: not asked for.  Zero in rows of padding, NaN in rows
  *           with a target that is no label (which count nowhere else).
  *   dw      [n_out, H] of the model's dtype, rows lddw >= H elements apart, or NULL;  db  [n_out] fp32, or NULL.  Written, not added to.
- * Outputs may not overlap inputs.  bf16 models: g is rounded to bf16 (it is an operand of tensor-core products); db, dx and dW are
+ * Outputs may not overlap inputs.  bf16 models: g is rounded to bf16 (it is an operand of tensor-core products, as in mixed-precision
+ * training; half a step is 2^-8 of it, and the same for every row whose weight and probability are the same); db, dx and dW are
  * accumulated in fp32, db from g as it was before that rounding.  Everything else is fp32 throughout.
  */
 wind_status_t wind_label_loss_grad(const wind_output_t* o, const void* x, int64_t ldx, const int32_t* target, int32_t N, const float* lse,

@@ -31,12 +31,13 @@
 // models) because it is a tensor-core operand; dx and dW are accumulated in fp32 and rounded once.
 //
 // What bounds it, loss and gradient together (B200; floor: 8 N H n_out operations at a large matrix product's 1625 TFLOP/s):
-//     4096 rows, H = 2048, 65536 outputs     3.4 to 3.5 ms, floor 2.7: the tensor cores under the power limit (3.2 at the rate that a
-//                                            matrix product keeps up for seconds)
+//     4096 rows, H = 2048, 65536 outputs     3.45 ms, floor 2.7: the tensor cores under the power limit (3.2 at the rate that a matrix product
+//                                            keeps up for seconds), and in the logits eight epilogue warps that hold sums in registers
 //     8003 rows, H = 1024, 8193 outputs      455 to 465 us, floor 298: the same, the epilogue of LOGITS, and last waves of equal tiles
-//     20011 rows (35 % padding), 640, 1025   112 us, floor 42: FORWARD 21, LOGITS 26 (exponentials and rounding, 6700 cycles a tile
-//                                            against 5200 of products), PRODUCTS 38, gathering 2 x 11.5 at 2.9 TB/s, joining and sums 11
-//     1 row, 1024, 8193 (loss)               12 us, floor 2.6: two launches, W read at 5 TB/s
+//     20011 rows (35 % padding), 640, 1025   112 us, floor 42: FORWARD 21, LOGITS 26 (6700 cycles of epilogue a tile, waits for tensor
+//                                            memory and between warps, against 5200 of products), PRODUCTS 38, gathering 2 x 11.5 at
+//                                            2.9 TB/s, joining and sums 11
+//     1 row, 1024, 8193 (loss)               12 us, floor 2.6: a chain of two kernels (11.3 in a graph of ten), W read at 5 TB/s
 //
 // Every wait on an mbarrier is bounded: after about two seconds the CTA marks the workspace as timed out, frees its tensor memory and returns.
 #include <cuda.h>
@@ -1557,7 +1558,8 @@ static int tile_cols(int row_tiles, int cols, int most) {
 // Two CTAs to a tile of 256 x 256 fetch a third less from L2 than a CTA to 128 x 256, and draw less power, but there are half as many
 // tiles to spread over the chip.  Logits: a text model's step (4096 rows, H = 2048, 65536 outputs) takes 3.50 ms with them and 3.65
 // without, the large vocabulary's logits (H = 1024) 102 us either way, the lattice's (H = 640) 30 us against 26.  Products: the large
-// vocabulary's 180 us against 189 (8003 rows, 512 tiles), 5 us lost with half the rows, the lattice's 47 us against 38.
+// vocabulary's 180 us against 189 (8003 rows, 512 tiles), 5 us lost with half the rows, the lattice's 47 us against 38.  (Between
+// these widths and numbers of tiles nothing was measured: the borders lie somewhere there.)
 static bool pairs_pay(int H, long long tiles) { return H >= 1536 && tiles >= 2 * kFillCtas; }
 static bool pairs_pay_products(int H, long long tiles) { return H >= 1024 && tiles >= 3 * kFillCtas; }
 
