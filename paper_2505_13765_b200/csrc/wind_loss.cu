@@ -550,12 +550,12 @@ struct LossGemm {
 // for six products of 128 x 128 x 64 (64 bytes of L2 a cycle and SM; a fetch for each product would be 128).
 template <int MODE, int KIND>
 struct Shape {
-    // Tensor cores cut where they add; over a long K that is up to 2^-24 an addition, all one way (a single row of H = 1024 had a loss
+    // Tensor cores cut where they add; over a long K that is up to 2^-23 an addition, all one way (a single row of H = 1024 had a loss
     // 3e-6 off).  Logits of fp32 models and of calls of few rows: an accumulator takes one K block, whose sum is added up in registers;
     // logits of long bf16 rows: sixteen of them, which takes FORWARD of 4096 x 2048 x 65536 from 648 to 673 us, LOGITS from 700 to 755 (eight
     // epilogue warps have room for the sums, sixteen do not); with eight K blocks an accumulator 717 and 852.
     static constexpr bool SUMS = KIND == F32 || ((KIND == BF16_FINE || KIND == BF16_LONG) && MODE != PRODUCTS);
-    static constexpr int ACC_BLOCKS = SUMS ? (KIND == BF16_LONG ? kLongBlocks : 1) : 1 << 30;         // K blocks that an accumulator takes
+    static constexpr int ACC_BLOCKS = SUMS ? (KIND == BF16_LONG ? kLongBlocks : 1) : 1 << 30;   // K blocks that an accumulator takes
     static constexpr int TN = SUMS && KIND != BF16_LONG ? 128 : 256;                         // most columns of a tile (BM = 128 rows)
     static constexpr int A_PARTS = KIND == F32 ? 3 : (KIND == BF16_FINE && MODE == PRODUCTS ? 2 : 1), B_PARTS = KIND == F32 ? 3 : 1;
     static constexpr int TERMS = KIND == F32 ? 6 : A_PARTS;
@@ -1619,7 +1619,7 @@ LossLayout loss_layout(const wind_output_t& o, int N, int K, int grad, bool most
         // 8 K blocks (bf16) at least, and none where the tiles alone are many.
         const int least_kb = cdiv(8, terms);
         // And of at most so many that a bf16 sum stays below kSumAdditions: the tensor cores cut, all one way (2^21 rows of positive
-        // activations in one accumulator: dW 1e-3 short).  (fp32 adds each K block up in registers.)
+        // activations in one accumulator: dW 0.9 % short).  (fp32 adds each K block up in registers.)
         const int most_kb = f32 ? 1 << 30 : kSumAdditions / (BK / 16) / L.kind;      // (a K block of the FINE kind is two terms long)
         const long long work = t_dx * kb_dx + t_dw * kb_dw, share = (2 * work + 3 * kFillCtas - 1) / (3 * kFillCtas);
         auto parts_of = [&](long long tiles, int kb) {
