@@ -144,3 +144,31 @@ def test_a_teacher_by_its_own_window_and_a_students_loss(pkg, dtype):  # noqa: F
     z = (c["x"].double() @ c["w"].double().T + c["b"].double())[rows] / 2
     want = 4 * (torch.special.xlogy(q, q) - q * torch.log_softmax(z, 1)).sum(1)
     assert bool(((got["loss"][rows].double() - want).abs() <= ref["tol_loss"]).all())
+
+
+def test_two_calls_at_once_in_every_form(pkg):  # noqa: F811
+    """Calls on streams of their own from threads of their own, each with its own workspace: pairs of CTAs, long rows, few rows, fp32."""
+    import threading
+    made = [make(30 + i, dtype, N, H, V, K, pad=0.1) for i, (dtype, N, H, V, K) in enumerate(
+        [("bf16", 900, 2048, 12289, 3), ("bf16", 1700, 1640, 5377, 0), ("bf16", 600, 1100, 1000, 0), ("f32", 500, 200, 3000, 0), ("bf16", 1, 1024, 8193, 0)])]
+    refs = [reference(c) for c in made]
+    torch.cuda.synchronize()
+    out = [None] * len(made)
+
+    def work(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            ws = pkg.alloc_loss_workspace(made[i]["w"], made[i]["x"].shape[0], made[i]["ids"].shape[1] if "ids" in made[i] else 0, True)
+            for _ in range(6):
+                out[i] = call(pkg, made[i], ws=ws, check=False)
+            assert pkg.wind_loss_status(ws, check=False) == 0
+        s.synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(made))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i, c in enumerate(made):
+        assert out[i] is not None
+        verify(out[i], refs[i], i)
